@@ -209,6 +209,105 @@ int emu_set_fallback(int mode);
 #define EMU_SGEMM_SPLIT_STREAMED 1
 int emu_set_sgemm_split(int mode);
 
+/* ---------------------------------------------------------------------------
+   Operators of a mixture-of-experts layer: the router, the products with the
+   experts' matrices (forward and gradients) and with 4-bit expert matrices.
+
+   Common to them.  A token t chooses k of E experts; the (token, choice) pairs
+   ordered by expert, then token, are the rows.  Element types are EMU_F32,
+   EMU_BF16 (bfloat16) and EMU_F16 (binary16) of all matrices of a call;
+   weights, their gradients and every sum are FP32, rounded once to the output's
+   type.  FP32 products are those of emu_sgemm: three BF16 components of each
+   operand, six component products, FP32 accumulation (so FP32 accuracy for
+   finite inputs of at least 2^-103 in magnitude; a non-finite entry makes its
+   outputs NaN).  They raise no EMU_STATUS_* bits.
+   Matrices are row-major with leading dimensions in elements, at any element's
+   alignment; index arrays are int32.  Device pointers, ordered on the current
+   stream, no host synchronisation; only emu_moe_route (more than 64 tokens)
+   and emu_q4_gemm (few rows) use the workspace.
+   offsets: E + 1 entries, rows [offsets[e], offsets[e + 1]) belong to expert e
+   (offsets[0] counts as 0); an expert may have none.  Rows from offsets[E] on
+   belong to no expert: their outputs are zero and their inputs are not used.
+   The values are read on the device and clamped to the rows that exist, so a
+   router's result is passed on without the host's knowledge.
+   rows: where given, row r of the product reads row rows[r] of X; an entry
+   outside X stands for a row of zeros.
+   EMU_EINVAL (before any HIP call) for a bad type, negative sizes, a leading
+   dimension below its row length, a NULL pointer to something that is not
+   empty, or sizes beyond the limits given.  At most 2^24 - 1 tokens, 2^31 - 1
+   rows and 2^30 - 1 columns; E at most 2^16. */
+#define EMU_F32 0
+#define EMU_BF16 1
+#define EMU_F16 2
+
+/* Router.  logits: T x E (ldl), 1 <= E <= 1024, 1 <= k <= min(E, 32).  ids
+   (T x k): the experts with the k largest logits in descending order, the
+   lowest index first among equal ones; -inf and NaN are never chosen, and -1
+   fills up where fewer than k are left (weight 0, no row).  weights (T x k,
+   FP32): exp(l - m) / S with m the token's largest logit and S the sum of the
+   exponentials over the chosen experts (EMU_ROUTE_CHOSEN) or over all
+   (EMU_ROUTE_ALL); experts at +inf share the weight.  offsets (E + 1); rows
+   (T k): the token of each row, -1 from offsets[E] on; slots (T x k): the row
+   of each choice, or -1.  The order is by expert, then token. */
+#define EMU_ROUTE_CHOSEN 0
+#define EMU_ROUTE_ALL 1
+int emu_moe_route(int dtype, int64_t T, int E, int k, int scope, const void *logits, int64_t ldl,
+                  int32_t *ids, float *weights, int32_t *offsets, int32_t *rows, int32_t *slots);
+/* Gradient of the logits (T x E, ldd, fully written) from the gradient of the
+   weights (T x k; the entries of ids = -1 are not used): w_j dw_j at the chosen
+   experts, minus p_e sum_j w_j dw_j, p the softmax over the scope's set.
+   logits are read in EMU_ROUTE_ALL only. */
+int emu_moe_route_grad(int dtype, int64_t T, int E, int k, int scope, const void *logits, int64_t ldl,
+                       const int32_t *ids, const float *weights, const float *dweights,
+                       void *dlogits, int64_t ldd);
+
+/* Y[t] = sum over j of weights[t, j] Z[slots[t, j]] (T x D, ldy); Z: R x D
+   (ldz).  A slot outside Z adds nothing, whatever its weight.  weights NULL
+   stands for ones (the gradient of reading token rows through `rows`).
+   1 <= k <= 32. */
+int emu_moe_combine(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *Z, int64_t ldz,
+                    const int32_t *slots, const float *weights, void *Y, int64_t ldy);
+/* Its gradients: dZ[slots[t, j]] = weights[t, j] dY[t], zero for the rows with
+   rows[r] < 0; dweights[t, j] = <Z[slots[t, j]], dY[t]>, 0 for a slot outside Z.
+   slots and rows (R entries) as emu_moe_route gives them. */
+int emu_moe_combine_grad(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *dY,
+                         int64_t lddy, const void *Z, int64_t ldz, const int32_t *slots,
+                         const float *weights, const int32_t *rows, void *dZ, int64_t lddz,
+                         float *dweights);
+
+/* Y[r] = X[rows[r]] op(W[e(r)]) for the R rows of Y (R x N, ldy), op(W) K x N:
+   W[e] starts at W + e stride and is K x N (ldw >= N) for transb 'N', N x K
+   (ldw >= K) for 'T'.  X: XR x K (ldx); rows NULL stands for the row itself
+   (XR >= R).  The gradient of the rows is the call with dY for X and the other
+   transb. */
+int emu_grouped_gemm(int dtype, char transb, int E, int64_t R, int64_t N, int64_t K, const void *X,
+                     int64_t ldx, int64_t XR, const int32_t *rows, const void *W, int64_t ldw,
+                     int64_t stride, const int32_t *offsets, void *Y, int64_t ldy);
+/* Gradient of the matrices: dW[e] = sum over the rows r of e of X[rows[r]]^T
+   dY[r], stored as W for the same transb (fully written; zeros for an expert
+   without rows). */
+int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64_t K, const void *X,
+                      int64_t ldx, int64_t XR, const int32_t *rows, const void *dY, int64_t lddy,
+                      const int32_t *offsets, void *dW, int64_t ldw, int64_t stride);
+
+/* Matrices in 4 bits.  W is E x N x K, contiguous; byte j of a row of Q (K / 2
+   bytes) holds entry 2 j in its low and 2 j + 1 in its high half, q in 0 .. 15.
+   Each `group` (32, 64 or 128) entries along K share a scale s, and where mins
+   is given an offset m, of the call's type (E x N x K / group):
+   W = s (q - 8), or s q + m.  K is a multiple of the group.
+   emu_q4_gemm: Y[r] = X[rows[r]] W[e(r)]^T for R rows ordered by expert as for
+   emu_grouped_gemm (offsets NULL: E = 1, every row); made for few rows of each
+   expert, where the bytes of Q bound it.  The products are formed with the exact
+   integers q on matrix instructions and scaled per group in FP32. */
+int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, const void *X,
+                int64_t ldx, int64_t XR, const int32_t *rows, const uint8_t *Q, const void *scales,
+                const void *mins, const int32_t *offsets, void *Y, int64_t ldy);
+/* Q and scales of `rows` rows of K entries (ldw): s = max |w| / 7 of the group,
+   rounded to the call's type, q = 8 + the integer nearest w / s (ties to even) within -8 .. 7 (8 where s = 0;
+   w must be finite). */
+int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, int64_t ldw, uint8_t *Q,
+                void *scales);
+
 /* Stream for subsequent calls (a hipStream_t); NULL selects the default
    stream.  Switching streams orders the new stream after the work already
    queued on the previous one (an event dependency, no host synchronisation),

@@ -15,11 +15,23 @@ library is not built, importing the functions raises.
     set_split_scope(scope)         -> SCOPE_OPERAND (default) or SCOPE_ROWCOL weights
     scale_exponents(X, by_col)     -> int32 tensor of the ROWCOL weights
     domain_status()                -> EMU_STATUS_* bits accumulated since last call
+
+Mixture-of-experts operators (float32, bfloat16 or float16; see emu.h):
+
+    moe_route(logits, k, scope)    -> Routing(ids, weights, offsets, rows, slots)
+    moe_route_grad(logits, ids, weights, dweights, scope) -> gradient of the logits
+    moe_combine(Z, slots, weights) -> weighted sum of each token's rows of Z
+    moe_combine_grad(dY, Z, slots, weights, rows) -> (dZ, dweights)
+    grouped_gemm(X, W, offsets, transb, rows)    -> Y[r] = X[rows[r]] op(W[expert of r])
+    grouped_wgrad(X, dY, offsets, transb, rows)  -> gradient of W
+    q4_pack(W, group)              -> (Q, scales): W in 4 bits
+    q4_gemm(X, Q, scales, mins, offsets, rows)   -> Y[r] = X[rows[r]] W[expert of r]^T
 """
 from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -42,7 +54,11 @@ EXPORTS = ("emu_sgemm", "emu_dgemm", "emu_set_stream", "emu_set_split_mode",
            "emu_domain_status", "emu_last_error", "emu_release_workspace",
            "emu_workspace_bytes", "emu_split_f32", "emu_split_f64", "emu_profile_enable",
            "emu_profile_read", "emu_set_split_scope", "emu_scale_exponents", "emu_sgemm_ex",
-           "emu_dgemm_ex", "emu_dgemm_noalloc", "emu_set_fallback", "emu_set_sgemm_split")
+           "emu_dgemm_ex", "emu_dgemm_noalloc", "emu_set_fallback", "emu_set_sgemm_split",
+           "emu_moe_route", "emu_moe_route_grad", "emu_moe_combine", "emu_moe_combine_grad",
+           "emu_grouped_gemm", "emu_grouped_wgrad", "emu_q4_gemm", "emu_q4_pack")
+ROUTE_SCOPES = {"chosen": 0, "all": 1}      # EMU_ROUTE_CHOSEN, EMU_ROUTE_ALL
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # EMU_F32, EMU_BF16, EMU_F16
 
 
 class EmuError(RuntimeError):
@@ -82,6 +98,20 @@ def lib() -> ctypes.CDLL:
         L.emu_split_f64.argtypes = [i64, i64, p, i64, ci, p, p]
         L.emu_profile_enable.argtypes = [ci]
         L.emu_profile_read.argtypes = [i64, p, p, ctypes.POINTER(ctypes.c_int64)]
+        L.emu_moe_route.argtypes = [ci, i64, ci, ci, ci, p, i64, p, p, p, p, p]
+        L.emu_moe_route_grad.argtypes = [ci, i64, ci, ci, ci, p, i64, p, p, p, p, i64]
+        L.emu_moe_combine.argtypes = [ci, i64, i64, ci, i64, p, i64, p, p, p, i64]
+        L.emu_moe_combine_grad.argtypes = [ci, i64, i64, ci, i64, p, i64, p, i64, p, p, p, p, i64, p]
+        L.emu_grouped_gemm.argtypes = [ci, ch, ci, i64, i64, i64, p, i64, i64, p, p, i64, i64, p, p,
+                                       i64]
+        L.emu_grouped_wgrad.argtypes = [ci, ch, ci, i64, i64, i64, p, i64, i64, p, p, i64, p, p, i64,
+                                        i64]
+        L.emu_q4_gemm.argtypes = [ci, ci, i64, i64, i64, ci, p, i64, i64, p, p, p, p, p, p, i64]
+        L.emu_q4_pack.argtypes = [ci, i64, i64, ci, p, i64, p, p]
+        for name in ("emu_moe_route", "emu_moe_route_grad", "emu_moe_combine",
+                     "emu_moe_combine_grad", "emu_grouped_gemm", "emu_grouped_wgrad",
+                     "emu_q4_gemm", "emu_q4_pack"):
+            getattr(L, name).restype = ci
         for name in ("emu_sgemm", "emu_dgemm", "emu_set_stream", "emu_set_split_mode",
                      "emu_domain_status", "emu_release_workspace", "emu_split_f32",
                      "emu_split_f64", "emu_profile_enable", "emu_profile_read",
@@ -228,6 +258,281 @@ def dgemm_ex(A, B, nprod, C=None, transa="N", transb="N", alpha=1.0, beta=0.0):
     """C = alpha op(A) op(B) + beta C in FP64 with nprod retained products."""
     return _gemm_ex(lib().emu_dgemm_ex, torch.float64, A, B, C, transa, transb, float(alpha),
                     float(beta), (int(nprod),))
+
+
+# ---------------------------------------------------------------------------
+# Mixture-of-experts operators.
+
+class Routing(NamedTuple):
+    """moe_route's result: T tokens, k choices, E experts (see emu_moe_route)."""
+    ids: torch.Tensor        # T x k, the experts in descending order, -1 for none
+    weights: torch.Tensor    # T x k, float32
+    offsets: torch.Tensor    # E + 1, first row of each expert
+    rows: torch.Tensor       # T k, the token of each row, -1 past the last
+    slots: torch.Tensor      # T x k, the row of each choice, -1 for none
+
+
+def _float_mat(t, name: str, like=None) -> int:
+    """The element code of a row-major matrix of a supported type."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    _layout(t, like.dtype if like is not None else t.dtype, name)
+    return _DTYPES[t.dtype]
+
+
+def _packed(t, name: str, dtype, shape):
+    """A contiguous tensor of this type and shape."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {' x '.join(map(str, shape))}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _experts(t, name: str, dtype):
+    """E, rows, columns, leading dimension and stride of E row-major matrices."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be a 3-D tensor")
+    E, a, b = t.shape
+    ld = t.stride(1) if a > 1 else b
+    if (b > 1 and t.stride(2) != 1) or ld < b or (E > 1 and t.stride(0) < 0):
+        raise ValueError(f"{name} must hold row-major matrices with unit column stride")
+    return E, a, b, max(1, ld), t.stride(0) if E > 1 else 0
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _launch(fn, device, *args):
+    """One call on the current stream of the operands' device."""
+    if device.index == torch.cuda.current_device():
+        _bind_stream(device)
+        _check(fn(*args))
+    else:
+        with torch.cuda.device(device):
+            _bind_stream(device)
+            _check(fn(*args))
+
+
+def _same_gpu(*named):
+    present = [(n, t) for n, t in named if t is not None]
+    _on_gpu(*present)
+    for n, t in present[1:]:
+        if t.device != present[0][1].device:
+            raise ValueError(f"{n} is on {t.device}, {present[0][0]} on {present[0][1].device}")
+
+
+def _scope(scope: str) -> int:
+    if scope not in ROUTE_SCOPES:
+        raise ValueError("scope must be 'chosen' or 'all'")
+    return ROUTE_SCOPES[scope]
+
+
+def moe_route(logits: torch.Tensor, k: int, scope: str = "chosen") -> Routing:
+    """The k experts of each token, their softmax weights over the chosen
+    experts or over all, and the rows' order by expert (see emu_moe_route)."""
+    code, how = _float_mat(logits, "logits"), _scope(scope)
+    T, E = logits.shape
+    _same_gpu(("logits", logits))
+    dev = logits.device
+    ids, rows, slots = (torch.empty(n, dtype=torch.int32, device=dev) for n in ((T, k), T * k, (T, k)))
+    offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
+    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    _launch(lib().emu_moe_route, dev, code, T, E, k, how, logits.data_ptr(), _ld(logits),
+            ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
+            slots.data_ptr())
+    return Routing(ids, weights, offsets, rows, slots)
+
+
+def moe_route_grad(logits, ids, weights, dweights, scope: str = "chosen") -> torch.Tensor:
+    """Gradient of the logits from the gradient of moe_route's weights."""
+    code, how = _float_mat(logits, "logits"), _scope(scope)
+    T, E = logits.shape
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids must be a T x k tensor")
+    k = ids.shape[1]
+    _packed(ids, "ids", torch.int32, (T, k))
+    _packed(weights, "weights", torch.float32, (T, k))
+    _packed(dweights, "dweights", torch.float32, (T, k))
+    _same_gpu(("logits", logits), ("ids", ids), ("weights", weights), ("dweights", dweights))
+    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    _launch(lib().emu_moe_route_grad, logits.device, code, T, E, k, how, logits.data_ptr(),
+            _ld(logits), ids.data_ptr(), weights.data_ptr(), dweights.data_ptr(), out.data_ptr(), E)
+    return out
+
+
+def _slots(slots, weights):
+    if not isinstance(slots, torch.Tensor) or slots.dim() != 2:
+        raise ValueError("slots must be a T x k tensor")
+    T, k = slots.shape
+    _packed(slots, "slots", torch.int32, (T, k))
+    if weights is not None:
+        _packed(weights, "weights", torch.float32, (T, k))
+    return T, k
+
+
+def moe_combine(Z, slots, weights=None, Y=None) -> torch.Tensor:
+    """Y[t] = sum over j of weights[t, j] Z[slots[t, j]] (weights None: ones)."""
+    code = _float_mat(Z, "Z")
+    T, k = _slots(slots, weights)
+    R, D = Z.shape
+    Y = _rows_out(Y, T, D, Z, "Y")
+    _same_gpu(("Z", Z), ("slots", slots), ("weights", weights), ("Y", Y))
+    _launch(lib().emu_moe_combine, Z.device, code, T, D, k, R, Z.data_ptr(), _ld(Z),
+            slots.data_ptr(), _ptr(weights), Y.data_ptr(), _ld(Y))
+    return Y
+
+
+def moe_combine_grad(dY, Z, slots, weights, rows):
+    """(dZ, dweights): the gradients of moe_combine; rows as moe_route gives them."""
+    code = _float_mat(Z, "Z")
+    _float_mat(dY, "dY", Z)
+    if weights is None:
+        raise TypeError("weights must be a torch.Tensor")
+    T, k = _slots(slots, weights)
+    R, D = Z.shape
+    if tuple(dY.shape) != (T, D):
+        raise ValueError(f"dY must be {T} x {D}, got {tuple(dY.shape)}")
+    _packed(rows, "rows", torch.int32, (R,))
+    _same_gpu(("Z", Z), ("dY", dY), ("slots", slots), ("weights", weights), ("rows", rows))
+    dZ = torch.empty((R, D), dtype=Z.dtype, device=Z.device)
+    dw = torch.empty((T, k), dtype=torch.float32, device=Z.device)
+    _launch(lib().emu_moe_combine_grad, Z.device, code, T, D, k, R, dY.data_ptr(), _ld(dY),
+            Z.data_ptr(), _ld(Z), slots.data_ptr(), weights.data_ptr(), rows.data_ptr(),
+            dZ.data_ptr(), max(1, D), dw.data_ptr())
+    return dZ, dw
+
+
+def _rows_out(Y, R: int, N: int, like, name: str):
+    """An output of R rows: allocated when None, else checked to be R x N."""
+    if Y is None:
+        return torch.empty((R, N), dtype=like.dtype, device=like.device)
+    _float_mat(Y, name, like)
+    if tuple(Y.shape) != (R, N):
+        raise ValueError(f"{name} must be {R} x {N}, got {tuple(Y.shape)}")
+    return Y
+
+
+def _grouping(X, offsets, rows, E: int, R=None) -> int:
+    """The number of rows of a grouped product, its index arrays checked."""
+    if offsets is not None:
+        _packed(offsets, "offsets", torch.int32, (E + 1,))
+    if rows is not None:
+        if not isinstance(rows, torch.Tensor) or rows.dim() != 1:
+            raise ValueError("rows must be a 1-D tensor")
+        _packed(rows, "rows", torch.int32, rows.shape)
+    n = X.shape[0] if rows is None else rows.shape[0]
+    if R is not None and n != R:
+        raise ValueError(f"{n} rows of X for {R} rows of the product")
+    return n
+
+
+def _transb(transb: str) -> bool:
+    if transb not in ("N", "T"):
+        raise ValueError("transb must be 'N' or 'T'")
+    return transb == "T"
+
+
+def grouped_gemm(X, W, offsets, Y=None, transb: str = "N", rows=None) -> torch.Tensor:
+    """Y[r] = X[r] op(W[e(r)]), or X[rows[r]]; rows ordered by expert, expert e
+    has the rows offsets[e] to offsets[e + 1].  W: E x K x N ("N") or E x N x K
+    ("T")."""
+    code, tb = _float_mat(X, "X"), _transb(transb)
+    E, a, b, ldw, stride = _experts(W, "W", X.dtype)
+    N, K = (a, b) if tb else (b, a)
+    if X.shape[1] != K:
+        raise ValueError("inner dimensions differ")
+    if offsets is None:
+        raise TypeError("offsets must be a torch.Tensor")
+    R = _grouping(X, offsets, rows, E)
+    Y = _rows_out(Y, R, N, X, "Y")
+    _same_gpu(("X", X), ("W", W), ("offsets", offsets), ("rows", rows), ("Y", Y))
+    _launch(lib().emu_grouped_gemm, X.device, code, transb.encode(), E, R, N, K, X.data_ptr(),
+            _ld(X), X.shape[0], _ptr(rows), W.data_ptr(), ldw, stride, offsets.data_ptr(),
+            Y.data_ptr(), _ld(Y))
+    return Y
+
+
+def grouped_wgrad(X, dY, offsets, dW=None, transb: str = "N", rows=None) -> torch.Tensor:
+    """dW[e] = sum over the rows r of expert e of X[r]^T dY[r] (X[rows[r]] with
+    rows), E x K x N for "N", its transpose E x N x K for "T"."""
+    code, tb = _float_mat(X, "X"), _transb(transb)
+    _float_mat(dY, "dY", X)
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("offsets must be a 1-D tensor of E + 1 entries")
+    E = offsets.shape[0] - 1
+    R, N, K = dY.shape[0], dY.shape[1], X.shape[1]
+    _grouping(X, offsets, rows, E, R)
+    shape = (E, N, K) if tb else (E, K, N)
+    if dW is None:
+        dW = torch.empty(shape, dtype=X.dtype, device=X.device)
+    elif tuple(dW.shape) != shape:
+        raise ValueError(f"dW must be {' x '.join(map(str, shape))}, got {tuple(dW.shape)}")
+    _, _, _, ldw, stride = _experts(dW, "dW", X.dtype)
+    _same_gpu(("X", X), ("dY", dY), ("offsets", offsets), ("rows", rows), ("dW", dW))
+    _launch(lib().emu_grouped_wgrad, X.device, code, transb.encode(), E, R, N, K, X.data_ptr(),
+            _ld(X), X.shape[0], _ptr(rows), dY.data_ptr(), _ld(dY), offsets.data_ptr(),
+            dW.data_ptr(), ldw, stride)
+    return dW
+
+
+def q4_pack(W: torch.Tensor, group: int = 64):
+    """(Q, scales) of E x N x K (or N x K) matrices: 4-bit entries, two to a byte
+    along K, and a scale for each group (see emu_q4_pack)."""
+    if not isinstance(W, torch.Tensor) or W.dim() not in (2, 3):
+        raise ValueError("W must be a 2-D or 3-D tensor")
+    lead, K = W.shape[:-1], W.shape[-1]
+    flat = W.reshape(-1, K)
+    code = _float_mat(flat, "W")
+    if group not in (32, 64, 128) or K % group:
+        raise ValueError("group must be 32, 64 or 128 and divide K")
+    _same_gpu(("W", W))
+    Q = torch.empty((*lead, K // 2), dtype=torch.uint8, device=W.device)
+    scales = torch.empty((*lead, K // group), dtype=W.dtype, device=W.device)
+    _launch(lib().emu_q4_pack, W.device, code, flat.shape[0], K, group, flat.data_ptr(), _ld(flat),
+            Q.data_ptr(), scales.data_ptr())
+    return Q, scales
+
+
+def q4_gemm(X, Q, scales, mins=None, offsets=None, rows=None, Y=None) -> torch.Tensor:
+    """Y[r] = X[r] W[e(r)]^T (X[rows[r]] with rows), W in 4 bits as q4_pack gives
+    it, with mins as W = scales q + mins.  Q: E x N x K/2; without offsets one
+    matrix (E = 1, or Q N x K/2) serves every row."""
+    code = _float_mat(X, "X")
+    if not isinstance(Q, torch.Tensor) or Q.dim() not in (2, 3):
+        raise ValueError("Q must be a 2-D or 3-D tensor")
+    E, N, half = (1, *Q.shape) if Q.dim() == 2 else Q.shape
+    K = X.shape[1]
+    if 2 * half != K:
+        raise ValueError("inner dimensions differ")
+    if offsets is None and E != 1:
+        raise ValueError("more than one matrix needs offsets")
+    _packed(Q, "Q", torch.uint8, Q.shape)
+    groups = scales.shape[-1] if isinstance(scales, torch.Tensor) and scales.dim() > 0 else 0
+    group = K // groups if groups else 0
+    if K and (group not in (32, 64, 128) or group * groups != K):
+        raise ValueError("scales must have K / 32, K / 64 or K / 128 columns")
+    _packed(scales, "scales", X.dtype, (*Q.shape[:-1], groups))
+    if mins is not None:
+        _packed(mins, "mins", X.dtype, scales.shape)
+    R = _grouping(X, offsets, rows, E)
+    Y = _rows_out(Y, R, N, X, "Y")
+    _same_gpu(("X", X), ("Q", Q), ("scales", scales), ("mins", mins), ("offsets", offsets),
+              ("rows", rows), ("Y", Y))
+    _launch(lib().emu_q4_gemm, X.device, code, E, R, N, K, group or 32, X.data_ptr(), _ld(X),
+            X.shape[0], _ptr(rows), Q.data_ptr(), scales.data_ptr(), _ptr(mins), _ptr(offsets),
+            Y.data_ptr(), _ld(Y))
+    return Y
 
 
 def split_f32(X: torch.Tensor, as_b: bool = False) -> torch.Tensor:

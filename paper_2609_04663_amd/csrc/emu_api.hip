@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "../../include/emu.h"
+#include "api_state.h"
 #include "emu_internal.h"
 
 namespace emu {
@@ -258,6 +259,18 @@ int check_gemm_args(bool ta, bool tb, int64_t M, int64_t N, int64_t K, const voi
 }
 
 }  // namespace
+
+namespace emu {
+hipStream_t api_stream() { return g_stream; }
+void api_clear_error() { g_err.clear(); }
+int api_fail(int code, const char *msg) { return fail(code, msg); }
+int api_hip_fail(hipError_t e, const char *what) { return hip_fail(e, what); }
+int api_workspace(size_t bytes, char **p) {
+    const int rc = ensure_workspace(bytes > 0 ? bytes : 1);
+    if (rc == EMU_OK) *p = g_ws.base + HDR;
+    return rc;
+}
+}  // namespace emu
 
 extern "C" {
 

@@ -1,0 +1,64 @@
+// Launch wrappers of the mixture-of-experts kernels (arguments checked by the
+// entry points in moe_api.hip).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace emu {
+
+constexpr int ROUTE_EXPERTS = 1024, ROUTE_CHOICES = 32;   // most experts, most choices of a token
+
+// Bytes of scratch that a routing of T tokens over E experts needs.
+size_t route_scratch(int64_t T, int E);
+hipError_t launch_route(int dtype, const void *logits, int64_t ld, int64_t T, int E, int k, bool all,
+                        int *ids, float *weights, int *offsets, int *rows, int *slots, char *scratch,
+                        hipStream_t s);
+hipError_t launch_route_grad(int dtype, const void *logits, int64_t ld, int64_t T, int E, int k,
+                             bool all, const int *ids, const float *weights, const float *dweights,
+                             void *dlogits, int64_t ldd, hipStream_t s);
+hipError_t launch_combine(int dtype, const void *Z, int64_t ldz, int64_t R, int64_t T, int64_t D,
+                          int k, const int *slots, const float *weights, void *Y, int64_t ldy,
+                          hipStream_t s);
+hipError_t launch_combine_grad(int dtype, const void *dY, int64_t lddy, const void *Z, int64_t ldz,
+                               int64_t R, int64_t T, int64_t D, int k, const int *slots,
+                               const float *weights, const int *rows, void *dZ, int64_t lddz,
+                               float *dweights, hipStream_t s);
+
+// Products of rows ordered by expert; see emu_grouped_gemm and emu_grouped_wgrad.
+struct GroupedGemm {
+    int dtype, E, N, K;
+    int64_t R, xrows;               // rows of the product; rows of X
+    const void *X, *W;
+    void *Y;
+    int64_t ldx, ldw, sw, ldy;
+    const int *offsets, *rows;
+    bool transb;
+};
+hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s);
+struct GroupedWgrad {
+    int dtype, E, M, N;             // dW[e] is M x N = sum over its rows of P[r]^T Q[r]
+    int64_t R, prows, qrows;
+    const void *P, *Q;
+    void *dW;
+    int64_t ldp, ldq, ldw, sw;
+    const int *offsets, *prow, *qrow;   // row numbers of P and Q, or null: r itself
+};
+hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s);
+
+// Products with 4-bit matrices; see emu_q4_gemm and emu_q4_pack.
+struct Q4Gemm {
+    int dtype, E, N, K, group;
+    int64_t R, xrows;
+    const void *X;
+    const uint8_t *Q;
+    const void *scales, *mins;
+    void *Y;
+    int64_t ldx, ldy;
+    const int *offsets, *rows;
+};
+hipError_t launch_q4_gemm(const Q4Gemm &g, hipStream_t s);
+hipError_t launch_q4_pack(int dtype, const void *W, int64_t rows, int64_t ldw, int K, int group,
+                          uint8_t *Q, void *scales, hipStream_t s);
+
+}  // namespace emu

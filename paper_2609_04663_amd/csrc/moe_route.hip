@@ -1,0 +1,371 @@
+// The router of a mixture of experts: each token's k experts with their
+// weights, the gradient of the logits, and the order of the rows by expert.
+//
+// Choice.  The k largest logits of a token in descending order, the lowest
+// index of equal ones first; -inf and NaN are never chosen.  With m the largest
+// logit, weights_j = exp(l_j - m) / sum exp(l - m), the sum over the chosen
+// experts or over all (a largest logit of +inf shares the weight among the
+// experts that have it).  Sixteen lanes hold a token's logits in registers, 16
+// values each at most (64 lanes above 256 experts); a round takes the largest
+// ordered bit pattern of the lanes, then the lowest index that has it, each
+// four DPP-style exchanges.  k rounds cost about 40 instructions each for four
+// tokens at once, less than the launch.
+//
+// Order.  Rows are ordered by expert, then token (a token's experts differ), a
+// stable order that no atomic decides: a workgroup of 64 tokens sets one bit
+// per token in a 64-bit mask of each expert, so a row's rank among its expert's
+// rows of the workgroup is a population count.  Up to 64 tokens that is the whole order, and
+// one launch does everything.  Beyond, the workgroups' counts are summed up by a second
+// kernel, and a third adds the ranks.
+#include "moe.h"
+#include "moe_common.h"
+
+namespace emu {
+namespace {
+
+constexpr int TOKENS = 64;          // tokens of a workgroup
+
+// Unsigned order of floats: larger value, larger number; -inf and NaN give 0.
+__device__ __forceinline__ unsigned ordered(float x) {
+    if (!(x > -INFINITY)) return 0u;
+    if (x == 0.0f) x = 0.0f;                                  // -0 equals 0
+    const unsigned u = __float_as_uint(x);
+    return (u & 0x80000000u) ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(unsigned o) {
+    return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o);
+}
+// exp(x - m) for x <= m; equal infinities give 1, -inf and NaN 0
+__device__ __forceinline__ float exp_below(float x, float m) {
+    return x == m ? 1.0f : (x > -INFINITY ? expf(x - m) : 0.0f);
+}
+
+template <int LANES, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, F f) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+
+// One token's choice by LANES lanes that hold the logits lane + LANES i in
+// x[i] (-inf past E).  Lane j % LANES of the group keeps choice j in slot
+// j / LANES of id and w; returns in *live how many were chosen.
+template <int LANES, int V>
+__device__ __forceinline__ void choose(const float (&x)[V], int sub, int k, bool all,
+                                       int (&id)[ROUTE_CHOICES / 16], float (&w)[ROUTE_CHOICES / 16]) {
+    unsigned o[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = ordered(x[i]);
+    constexpr int SLOTS = ROUTE_CHOICES / 16;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        id[s] = -1;
+        w[s] = -INFINITY;
+    }
+    float m = 0.0f;
+    for (int j = 0; j < k; ++j) {
+        unsigned best = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) best = o[i] > best ? o[i] : best;
+        best = over_lanes<LANES>(best, [](unsigned a, unsigned b) { return a > b ? a : b; });
+        if (best == 0) break;                                 // no expert is left
+        int at = 0x7FFFFFFF;
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i) at = o[i] == best ? sub + LANES * i : at;
+        at = over_lanes<LANES>(at, [](int a, int b) { return a < b ? a : b; });
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = at == sub + LANES * i ? 0u : o[i];
+        const float v = unordered(best);
+        if (j == 0) m = v;
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s)
+            if (j % LANES == sub && j / LANES == s) {
+                id[s] = at;
+                w[s] = v;
+            }
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) w[s] = id[s] >= 0 ? exp_below(w[s], m) : 0.0f;
+    if (all) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum += exp_below(x[i], m);
+    } else {
+#pragma unroll
+        for (int s = 0; s < SLOTS; ++s) sum += w[s];
+    }
+    sum = over_lanes<LANES>(sum, [](float a, float b) { return a + b; });
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) w[s] = id[s] >= 0 ? w[s] / sum : 0.0f;
+}
+
+template <int LANES, int V, typename T>
+__device__ __forceinline__ void load_logits(const T *row, int E, int sub, bool live, float (&x)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = sub + LANES * i;
+        x[i] = live && e < E ? (float)row[e] : -INFINITY;
+    }
+}
+
+// Exclusive sums of the E counts f(e) by the whole workgroup of 1024 threads,
+// E <= 1024; returns the sum below e = threadIdx.x, the total in *total.
+template <typename F>
+__device__ int sums_below(int E, F f, int *part, int *total) {
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+    const int n = e < E ? f(e) : 0;
+    int v = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int up = __shfl_up(v, d);
+        if (lane >= d) v += up;
+    }
+    if (lane == 63) part[wave] = v;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < 16; ++i) {
+        before += i < wave ? part[i] : 0;
+        all += part[i];
+    }
+    *total = all;
+    return before + v - n;
+}
+
+// One workgroup for 64 tokens.  One workgroup in all: the order too.
+template <typename T, int LANES, int V>
+__global__ __launch_bounds__(1024) void route_kernel(const T *__restrict__ logits, int64_t ld,
+                                                     int64_t tokens, int E, int k, int all,
+                                                     int *__restrict__ ids, float *__restrict__ weights,
+                                                     int *__restrict__ counts, int *__restrict__ offsets,
+                                                     int *__restrict__ rows, int *__restrict__ slots) {
+    __shared__ unsigned long long mask[ROUTE_EXPERTS];
+    __shared__ int start[ROUTE_EXPERTS], part[16];
+    const int tid = threadIdx.x, sub = tid % LANES;
+    if (tid < E) mask[tid] = 0;
+    __syncthreads();
+    constexpr int AT_ONCE = 1024 / LANES;
+    const bool single = gridDim.x == 1;
+    int id[TOKENS / AT_ONCE][ROUTE_CHOICES / 16];
+#pragma unroll
+    for (int p = 0; p < TOKENS / AT_ONCE; ++p) {
+        const int local = p * AT_ONCE + tid / LANES;
+        const int64_t t = (int64_t)blockIdx.x * TOKENS + local;
+        const bool live = t < tokens;
+        float x[V], w[ROUTE_CHOICES / 16];
+        load_logits<LANES, V>(logits + (live ? t : 0) * ld, E, sub, live, x);
+        choose<LANES, V>(x, sub, k, all, id[p], w);
+#pragma unroll
+        for (int s = 0; s < ROUTE_CHOICES / 16; ++s) {
+            const int j = sub + LANES * s;
+            if (!live || j >= k) continue;
+            ids[t * k + j] = id[p][s];
+            weights[t * k + j] = w[s];
+            if (id[p][s] >= 0) atomicOr(&mask[id[p][s]], 1ull << local);
+        }
+    }
+    __syncthreads();
+    if (!single) {
+        for (int e = tid; e < E; e += 1024)
+            counts[(int64_t)blockIdx.x * E + e] = __popcll(mask[e]);
+        return;
+    }
+    int total;
+    const int below = sums_below(E, [&](int e) { return __popcll(mask[e]); }, part, &total);
+    if (tid < E) {
+        start[tid] = below;
+        offsets[tid] = below;
+    }
+    if (tid == 0) offsets[E] = total;
+    __syncthreads();
+#pragma unroll
+    for (int p = 0; p < TOKENS / AT_ONCE; ++p) {
+        const int t = p * AT_ONCE + tid / LANES;
+#pragma unroll
+        for (int s = 0; s < ROUTE_CHOICES / 16; ++s) {
+            const int j = sub + LANES * s, e = id[p][s];
+            if (t >= tokens || j >= k) continue;
+            const int at = e < 0 ? -1 : start[e] + __popcll(mask[e] & ((1ull << t) - 1));
+            slots[t * k + j] = at;
+            if (at >= 0) rows[at] = t;
+        }
+    }
+    for (int i = total + tid; i < (int)tokens * k; i += 1024) rows[i] = -1;
+}
+
+// The counts of the workgroups of one expert become the sums of those before;
+// the expert's total goes to totals[e].  A workgroup for 16 experts: 64 lanes
+// walk the workgroups' counts of each.
+__global__ __launch_bounds__(1024) void route_sums_kernel(int *__restrict__ counts, int64_t blocks,
+                                                          int E, int *__restrict__ totals) {
+    const int lane = threadIdx.x & 63, e = blockIdx.x * 16 + (threadIdx.x >> 6);
+    if (e >= E) return;
+    int before = 0;
+    for (int64_t b0 = 0; b0 < blocks; b0 += 64) {
+        const int64_t b = b0 + lane;
+        const int n = b < blocks ? counts[b * E + e] : 0;
+        int v = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int up = __shfl_up(v, d);
+            if (lane >= d) v += up;
+        }
+        if (b < blocks) counts[b * E + e] = before + v - n;
+        before += __shfl(v, 63);
+    }
+    if (lane == 0) totals[e] = before;
+}
+
+// Slots and rows of 64 tokens, from their experts and the sums of the counts.
+__global__ __launch_bounds__(1024) void route_order_kernel(const int *__restrict__ ids, int64_t tokens,
+                                                           int E, int k, const int *__restrict__ counts,
+                                                           const int *__restrict__ totals,
+                                                           int *__restrict__ offsets,
+                                                           int *__restrict__ rows,
+                                                           int *__restrict__ slots) {
+    __shared__ unsigned long long mask[ROUTE_EXPERTS];
+    __shared__ int start[ROUTE_EXPERTS], part[16];
+    const int tid = threadIdx.x;
+    const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
+    const int n = (int)((tokens - t0 < TOKENS ? tokens - t0 : TOKENS) * k);
+    if (tid < E) mask[tid] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += 1024) {
+        const int e = ids[t0 * k + i];
+        if (e >= 0) atomicOr(&mask[e], 1ull << (i / k));
+    }
+    int total;
+    const int below = sums_below(E, [&](int e) { return totals[e]; }, part, &total);
+    if (tid < E) {
+        start[tid] = below + counts[(int64_t)blockIdx.x * E + tid];
+        if (blockIdx.x == 0) offsets[tid] = below;
+    }
+    if (blockIdx.x == 0 && tid == 0) offsets[E] = total;
+    __syncthreads();
+    for (int i = tid; i < n; i += 1024) {
+        const int e = ids[t0 * k + i], t = i / k;
+        const int at = e < 0 ? -1 : start[e] + __popcll(mask[e] & ((1ull << t) - 1));
+        slots[t0 * k + i] = at;
+        if (at >= 0) rows[at] = (int)(t0 + t);
+        if (t0 * k + i >= total) rows[t0 * k + i] = -1;
+    }
+}
+
+// Gradient of the logits: with p the softmax that gave the weights (0 outside
+// its set) and dw the weights' gradient, dl_e = [e chosen] p_e dw_e - p_e sum_j
+// w_j dw_j.  LANES lanes take a token.
+template <typename T, int LANES, int V>
+__global__ __launch_bounds__(256) void route_grad_kernel(const T *__restrict__ logits, int64_t ld,
+                                                         int64_t tokens, int E, int k, int all,
+                                                         const int *__restrict__ ids,
+                                                         const float *__restrict__ weights,
+                                                         const float *__restrict__ dweights,
+                                                         T *__restrict__ dlogits, int64_t ldd) {
+    const int sub = threadIdx.x % LANES;
+    const int64_t t = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const bool live = t < tokens;
+    const int64_t tc = live ? t : 0;
+    constexpr int SLOTS = ROUTE_CHOICES / 16;
+    int id[SLOTS];
+    float wd[SLOTS], w[SLOTS], mean = 0.0f;
+#pragma unroll
+    for (int s = 0; s < SLOTS; ++s) {
+        const int j = sub + LANES * s;
+        id[s] = j < k ? ids[tc * k + j] : -1;
+        w[s] = id[s] >= 0 ? weights[tc * k + j] : 0.0f;
+        wd[s] = id[s] >= 0 ? w[s] * dweights[tc * k + j] : 0.0f;
+        mean += wd[s];
+    }
+    mean = over_lanes<LANES>(mean, [](float a, float b) { return a + b; });
+    float x[V], m = -INFINITY, sum = 0.0f;
+    if (all) {
+        load_logits<LANES, V>(logits + tc * ld, E, sub, true, x);
+#pragma unroll
+        for (int i = 0; i < V; ++i) m = x[i] > m ? x[i] : m;
+        m = over_lanes<LANES>(m, [](float a, float b) { return a > b ? a : b; });
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = m > -INFINITY ? exp_below(x[i], m) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) sum += x[i];
+        sum = over_lanes<LANES>(sum, [](float a, float b) { return a + b; });
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = sum > 0.0f ? -x[i] / sum * mean : 0.0f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[i] = 0.0f;
+    }
+    for (int j = 0; j < k; ++j) {
+        const int from = (threadIdx.x & 63 & ~(LANES - 1)) + j % LANES, s = j / LANES;
+        const int e = __shfl(s == 0 ? id[0] : id[SLOTS - 1], from);
+        const float g = __shfl(s == 0 ? wd[0] - (all ? 0.0f : w[0] * mean)
+                                      : wd[SLOTS - 1] - (all ? 0.0f : w[SLOTS - 1] * mean),
+                               from);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (e == sub + LANES * i) x[i] += g;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int e = sub + LANES * i;
+        if (live && e < E) dlogits[t * ldd + e] = (T)x[i];
+    }
+}
+static_assert(ROUTE_CHOICES == 32, "two slots of a lane");
+
+// f<LANES, V>() with the fewest registers that hold E logits.
+template <typename F>
+void with_shape(int E, F &&f) {
+    using std::integral_constant;
+    if (E <= 64) f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+    else if (E <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+    else if (E <= 256) f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
+}
+
+int64_t route_blocks(int64_t T) { return T > TOKENS ? (T + TOKENS - 1) / TOKENS : 1; }
+
+}  // namespace
+
+size_t route_scratch(int64_t T, int E) {
+    const int64_t b = route_blocks(T);
+    return b > 1 ? (size_t)(b + 1) * E * sizeof(int) : 0;
+}
+
+hipError_t launch_route(int dtype, const void *logits, int64_t ld, int64_t T, int E, int k, bool all,
+                        int *ids, float *weights, int *offsets, int *rows, int *slots, char *scratch,
+                        hipStream_t s) {
+    const int64_t blocks = route_blocks(T);
+    int *const counts = reinterpret_cast<int *>(scratch), *const totals = counts + blocks * E;
+    with_type(dtype, [&](auto z) {
+        using type = decltype(z);
+        with_shape(E, [&](auto lanes, auto v) {
+            route_kernel<type, lanes, v><<<(unsigned)blocks, 1024, 0, s>>>(
+                static_cast<const type *>(logits), ld, T, E, k, all, ids, weights, counts, offsets,
+                rows, slots);
+        });
+    });
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || blocks == 1) return e;
+    route_sums_kernel<<<(E + 15) / 16, 1024, 0, s>>>(counts, blocks, E, totals);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    route_order_kernel<<<(unsigned)blocks, 1024, 0, s>>>(ids, T, E, k, counts, totals, offsets, rows,
+                                                         slots);
+    return hipGetLastError();
+}
+
+hipError_t launch_route_grad(int dtype, const void *logits, int64_t ld, int64_t T, int E, int k,
+                             bool all, const int *ids, const float *weights, const float *dweights,
+                             void *dlogits, int64_t ldd, hipStream_t s) {
+    with_type(dtype, [&](auto z) {
+        using type = decltype(z);
+        with_shape(E, [&](auto lanes, auto v) {
+            constexpr int per = 256 / decltype(lanes)::value;
+            route_grad_kernel<type, lanes, v><<<(unsigned)((T + per - 1) / per), 256, 0, s>>>(
+                static_cast<const type *>(logits), ld, T, E, k, all, ids, weights, dweights,
+                static_cast<type *>(dlogits), ldd);
+        });
+    });
+    return hipGetLastError();
+}
+
+}  // namespace emu
