@@ -311,8 +311,10 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
 /* Stream for subsequent calls (a hipStream_t); NULL selects the default
    stream.  Switching streams orders the new stream after the work already
    queued on the previous one (an event dependency, no host synchronisation),
-   since every call uses the one workspace.  EMU_OK, or EMU_EHIP if the event
-   calls fail. */
+   since every call uses the one workspace; not so a stream under capture,
+   where the caller orders the graph's launches.  A captured call must find the
+   workspace grown already (by the same call before the capture).  EMU_OK, or
+   EMU_EHIP if the event calls fail. */
 int emu_set_stream(void *hip_stream);
 
 /* Projection constant of the FP64 split for subsequent emu_dgemm and

@@ -276,10 +276,19 @@ extern "C" {
 
 int emu_set_stream(void *hip_stream) {
     const hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-    if (s != g_stream && g_ws.base) {
+    bool capturing = false;
+    if (s != g_stream && s != nullptr) {
+        hipStreamCaptureStatus state = hipStreamCaptureStatusNone;
+        const hipError_t e = hipStreamIsCapturing(s, &state);
+        if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+        capturing = state == hipStreamCaptureStatusActive;
+    }
+    if (s != g_stream && g_ws.base && !capturing) {
         // Every call shares the one workspace: work queued on the new stream
         // must not start before the calls already queued on the old one are
-        // done with it.  An event dependency, no host synchronisation.
+        // done with it.  An event dependency, no host synchronisation.  (A
+        // stream under capture runs nothing now and cannot wait for outside
+        // work; whoever launches the graph orders it.)
         if (!g_switch_event) {
             hipError_t e = hipEventCreateWithFlags(&g_switch_event, hipEventDisableTiming);
             if (e != hipSuccess) {
