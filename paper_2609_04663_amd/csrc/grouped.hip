@@ -279,7 +279,7 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_gemm_kernel(
     const T *__restrict__ W, int64_t ldw, int64_t sw, const int *__restrict__ offsets, int E, int64_t R,
     T *__restrict__ Y, int64_t ldy, int N, int K) {
     __shared__ __attribute__((aligned(16))) char lds[stage_bytes<T, BM>()];
-    const RowTile t = find_row_tile(offsets, E, R, BM, (N + BN - 1) / BN, blockIdx.x, true);
+    const RowTile t = RowTiles(offsets, E, R, BM, (N + BN - 1) / BN).of_workgroup(blockIdx.x);
     if (t.e < 0) return;
     const int64_t n0 = (int64_t)t.col * BN;
     T *const C = Y + t.first * ldy + n0;
@@ -317,6 +317,8 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_wgrad_kernel(
 }  // namespace
 
 hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s) {
+    if (direct_gemm(g) && g.R > 32 * (int64_t)g.E)
+        return launch_direct_gemm(g, g.R >= 512 * (int64_t)g.E ? 256 : 128, s);
     auto run = [&](auto z, auto bm, auto cb) {
         using T = decltype(z);
         constexpr int BM = decltype(bm)::value;
@@ -337,6 +339,7 @@ hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s) {
 }
 
 hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
+    if (direct_wgrad(g)) return launch_direct_wgrad(g, g.M >= 512 && g.N >= 512 ? 256 : 128, s);
     const int64_t tiles = (int64_t)g.E * ((g.M + 127) / 128) * ((g.N + BN - 1) / BN);
     with_type(g.dtype, [&](auto z) {
         using T = decltype(z);

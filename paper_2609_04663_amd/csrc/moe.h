@@ -46,6 +46,18 @@ struct GroupedWgrad {
 };
 hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s);
 
+// The kernels of 16-bit operands copied straight to LDS: whether a call can take
+// them, and their launches with square output tiles of 128 or 256.
+bool direct_gemm(const GroupedGemm &g);
+bool direct_wgrad(const GroupedWgrad &g);
+hipError_t launch_direct_gemm(const GroupedGemm &g, int tile, hipStream_t s);
+hipError_t launch_direct_wgrad(const GroupedWgrad &g, int tile, hipStream_t s);
+// one source file each: they take long to compile
+hipError_t launch_gemm16_bf16(const GroupedGemm &g, int tile, hipStream_t s);
+hipError_t launch_gemm16_f16(const GroupedGemm &g, int tile, hipStream_t s);
+hipError_t launch_wgrad16_bf16(const GroupedWgrad &g, int tile, hipStream_t s);
+hipError_t launch_wgrad16_f16(const GroupedWgrad &g, int tile, hipStream_t s);
+
 // Products with 4-bit matrices; see emu_q4_gemm and emu_q4_pack.
 struct Q4Gemm {
     int dtype, E, N, K, group;

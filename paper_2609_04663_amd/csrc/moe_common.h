@@ -63,6 +63,21 @@ inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
     return R / rows + (E + 1 < R ? E + 1 : R);
 }
 
+// A value that all lanes hold, below 2^31, in a scalar register.
+__device__ __forceinline__ int uniform(int64_t v) { return __builtin_amdgcn_readfirstlane((int)v); }
+
+// v summed over the lanes of the wave up to this one, in register moves between lanes
+// (rows of 16 lanes, then the last lane of one or two rows to those behind).
+__device__ __forceinline__ int sum_up_to_lane(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);     // row_shr 1
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);     // row_shr 2
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);     // row_shr 4
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);     // row_shr 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);     // row_bcast 15
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);     // row_bcast 31
+    return v;
+}
+
 // A workgroup's block of rows and its column tile.
 struct RowTile {
     int e;                 // expert; -1: there is no such tile; E: rows of no expert
@@ -70,53 +85,70 @@ struct RowTile {
     int col;               // column tile, 0 <= col < cols
 };
 
-// Tile `id` of an order that walks the experts, in each the column tiles, and
-// in each of those the expert's row blocks: neighbours share the columns of one
-// expert's matrix.  With xcd the workgroup number is first remapped (workgroup i
-// runs on XCD i % 8) so that each XCD takes a contiguous run of tiles.  Called
-// by all 64 lanes of a wave with the same arguments.
-__device__ inline RowTile find_row_tile(const int *__restrict__ offsets, int E, int64_t R, int rows,
-                                        int cols, int64_t id, bool xcd) {
-    const int lane = threadIdx.x & 63;
-    auto blocks_of = [&](int e) -> int64_t {
+// The row tiles of a product, in an order that walks the experts, in each groups
+// of eight row blocks, in each of those the column tiles, then the row blocks:
+// the tiles that run at a time share few rows and few columns of one expert.
+// Used by all 64 lanes of a wave with the same arguments; the first 64 experts'
+// blocks are counted once.
+struct RowTiles {
+    const int *offsets;
+    int E, rows, cols;
+    int64_t R;
+    int n0, upto0;                  // blocks of expert `lane`, and of those up to it
+    int64_t total;                  // tiles
+
+    __device__ __forceinline__ int blocks_of(int e) const {
         if (e > E) return 0;
         int64_t lo, hi;
         expert_rows(offsets, E, R, e, lo, hi);
-        return (hi - lo + rows - 1) / rows;
-    };
-    auto inclusive = [&](int64_t v) {
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t up = __shfl_up(v, d);
-            if (lane >= d) v += up;
-        }
-        return v;
-    };
-    if (xcd) {
-        int64_t total = 0;
-        for (int e0 = 0; e0 <= E; e0 += 64) total += __shfl(inclusive(blocks_of(e0 + lane)), 63);
+        return ((int)(hi - lo) + rows - 1) / rows;
+    }
+    __device__ __forceinline__ RowTiles(const int *offsets_, int E_, int64_t R_, int rows_, int cols_)
+        : offsets(offsets_), E(E_), rows(rows_), cols(cols_), R(R_) {
+        const int lane = threadIdx.x & 63;
+        n0 = blocks_of(lane);
+        upto0 = sum_up_to_lane(n0);
+        total = __builtin_amdgcn_readlane(upto0, 63);
+        for (int e0 = 64; e0 <= E; e0 += 64)
+            total += __builtin_amdgcn_readlane(sum_up_to_lane(blocks_of(e0 + lane)), 63);
         total *= cols;
-        const int64_t per = (total + 7) / 8;
-        if (id / 8 >= per) return {-1, 0, 0, 0};
-        id = id % 8 * per + id / 8;
-        if (id >= total) return {-1, 0, 0, 0};
     }
-    int64_t before = 0;
-    for (int e0 = 0; e0 <= E; e0 += 64) {
-        const int64_t n = blocks_of(e0 + lane), upto = inclusive(n);
-        const unsigned long long past = __ballot(id < (before + upto) * cols);
-        if (past != 0) {
-            const int at = __ffsll(past) - 1;
-            const int64_t n_e = __shfl(n, at), start = before + __shfl(upto, at) - n_e;
-            const int64_t r = id - start * cols;
-            int64_t lo, hi;
-            expert_rows(offsets, E, R, e0 + at, lo, hi);
-            const int64_t first = lo + r % n_e * rows;
-            return {e0 + at, first, first + rows < hi ? first + rows : hi, (int)(r / n_e)};
+    // the tile of workgroup w: workgroup w runs on XCD w % 8, and an XCD takes a
+    // contiguous run of tiles
+    __device__ __forceinline__ RowTile of_workgroup(int64_t w) const {
+        const int64_t per = (total + 7) / 8, id = w % 8 * per + w / 8;
+        if (w / 8 >= per || id >= total) return {-1, 0, 0, 0};
+        return at(id);
+    }
+    __device__ __forceinline__ RowTile at(int64_t id) const {
+        const RowTile t = search(id);
+        return {uniform(t.e), uniform(t.first), uniform(t.end), uniform(t.col)};
+    }
+    __device__ inline RowTile search(int64_t id) const {
+        const int lane = threadIdx.x & 63;
+        int n = n0, upto = upto0;
+        int64_t before = 0;
+        for (int e0 = 0;;) {
+            const unsigned long long past = __ballot(id < (before + upto) * cols);
+            if (past != 0) {
+                const int i = __ffsll(past) - 1;
+                const int n_e = __builtin_amdgcn_readlane(n, i);
+                const int64_t start = before + __builtin_amdgcn_readlane(upto, i) - n_e;
+                const int r = (int)(id - start * cols);
+                int64_t lo, hi;
+                expert_rows(offsets, E, R, e0 + i, lo, hi);
+                const int g0 = r / (8 * cols) * 8, in = r - g0 * cols;
+                const int high = n_e - g0 < 8 ? n_e - g0 : 8;
+                const int64_t first = lo + (int64_t)(g0 + in % high) * rows;
+                return {e0 + i, first, first + rows < hi ? first + rows : hi, in / high};
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+            e0 += 64;
+            if (e0 > E) return {-1, 0, 0, 0};
+            n = blocks_of(e0 + lane);
+            upto = sum_up_to_lane(n);
         }
-        before += __shfl(upto, 63);
     }
-    return {-1, 0, 0, 0};
-}
+};
 
 }  // namespace emu

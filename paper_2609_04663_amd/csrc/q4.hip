@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(
     constexpr int PL = Q4Elem<T>::PLANES;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int wn = WAVES / wk, cols = 16 * wn;
-    const RowTile t = find_row_tile(offsets, E, R, 16 * MT, (N + cols - 1) / cols, blockIdx.x, false);
+    const RowTile t = RowTiles(offsets, E, R, 16 * MT, (N + cols - 1) / cols).at(blockIdx.x);
     if (t.e < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int my_n = wave % wn, my_k = wave / wn, h = lane >> 4;
