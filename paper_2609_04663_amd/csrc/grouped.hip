@@ -33,6 +33,7 @@ template <typename T>
 using frag = T __attribute__((ext_vector_type(8)));
 
 constexpr int BN = 128, THREADS = 256;
+constexpr int64_t OFFSETS = (int64_t)1 << 31;        // leading dimensions that the FP32 kernels take
 
 template <typename T>
 struct Elem {
@@ -319,6 +320,7 @@ __global__ __launch_bounds__(THREADS, 2) void grouped_wgrad_kernel(
 hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s) {
     if (direct_gemm(g) && g.R > 32 * (int64_t)g.E)
         return launch_direct_gemm(g, g.R >= 512 * (int64_t)g.E ? 256 : 128, s);
+    if (g.dtype == EMU_F32 && g.R >= 64 * (int64_t)g.E && g.ldw < OFFSETS) return launch_gemm32(g, s);
     auto run = [&](auto z, auto bm, auto cb) {
         using T = decltype(z);
         constexpr int BM = decltype(bm)::value;
@@ -340,6 +342,7 @@ hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s) {
 
 hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
     if (direct_wgrad(g)) return launch_direct_wgrad(g, g.M >= 512 && g.N >= 512 ? 256 : 128, s);
+    if (g.dtype == EMU_F32 && g.ldp < OFFSETS && g.ldq < OFFSETS) return launch_wgrad32(g, s);
     const int64_t tiles = (int64_t)g.E * ((g.M + 127) / 128) * ((g.N + BN - 1) / BN);
     with_type(g.dtype, [&](auto z) {
         using T = decltype(z);

@@ -57,6 +57,9 @@ hipError_t launch_gemm16_bf16(const GroupedGemm &g, int tile, hipStream_t s);
 hipError_t launch_gemm16_f16(const GroupedGemm &g, int tile, hipStream_t s);
 hipError_t launch_wgrad16_bf16(const GroupedWgrad &g, int tile, hipStream_t s);
 hipError_t launch_wgrad16_f16(const GroupedWgrad &g, int tile, hipStream_t s);
+// The kernels of FP32 operands on tiles of 256 x 128.
+hipError_t launch_gemm32(const GroupedGemm &g, hipStream_t s);
+hipError_t launch_wgrad32(const GroupedWgrad &g, hipStream_t s);
 
 // Products with 4-bit matrices; see emu_q4_gemm and emu_q4_pack.
 struct Q4Gemm {
