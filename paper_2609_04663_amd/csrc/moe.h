@@ -73,6 +73,9 @@ struct Q4Gemm {
     const int *offsets, *rows;
 };
 hipError_t launch_q4_gemm(const Q4Gemm &g, hipStream_t s);
+hipError_t launch_q4_gemm_f32(const Q4Gemm &g, hipStream_t s);
+hipError_t launch_q4_gemm_bf16(const Q4Gemm &g, hipStream_t s);
+hipError_t launch_q4_gemm_f16(const Q4Gemm &g, hipStream_t s);
 hipError_t launch_q4_pack(int dtype, const void *W, int64_t rows, int64_t ldw, int K, int group,
                           uint8_t *Q, void *scales, hipStream_t s);
 
