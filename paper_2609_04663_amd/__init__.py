@@ -129,7 +129,8 @@ def _check(rc: int):
 
 
 def _bind_stream(dev: torch.device):
-    lib().emu_set_stream(ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream))
+    # the handle alone: a torch.cuda.Stream object costs 2 us to make
+    lib().emu_set_stream(torch._C._cuda_getCurrentRawStream(dev.index))
 
 
 def _layout(t: torch.Tensor, dtype, name: str):
@@ -140,8 +141,9 @@ def _layout(t: torch.Tensor, dtype, name: str):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     # the stride of a dimension of extent 1 is never used (NumPy-made tensors
     # of shape (1, n) can carry a row stride of 1)
-    if (t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1)
-            or (t.shape[0] > 1 and t.stride(0) < max(1, t.shape[1]))):
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 2 or (shape[1] > 1 and stride[1] != 1)
+            or (shape[0] > 1 and stride[0] < max(1, shape[1]))):
         raise ValueError(f"{name} must be a row-major 2-D tensor with unit column stride")
     return t
 
@@ -170,9 +172,10 @@ def _out(C, M: int, N: int, dtype, device):
 
 
 def _ld(t: torch.Tensor) -> int:
-    if t.shape[0] <= 1:
-        return max(1, t.shape[1])
-    return max(1, t.stride(0), t.shape[1])
+    rows, cols = t.shape
+    if rows <= 1:
+        return max(1, cols)
+    return max(1, t.stride(0), cols)
 
 
 def sgemm(A: torch.Tensor, B: torch.Tensor, C: torch.Tensor | None = None) -> torch.Tensor:
@@ -276,22 +279,24 @@ def _float_mat(t, name: str, like=None) -> int:
     """The element code of a row-major matrix of a supported type."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dtype not in _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    _layout(t, like.dtype if like is not None else t.dtype, name)
-    return _DTYPES[t.dtype]
+    _layout(t, t.dtype if like is None else like.dtype, name)
+    return code
 
 
 def _packed(t, name: str, dtype, shape):
-    """A contiguous tensor of this type and shape."""
+    """A contiguous tensor of this type and shape (a tuple)."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {' x '.join(map(str, shape))}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _experts(t, name: str, dtype):
@@ -317,19 +322,26 @@ def _launch(fn, device, *args):
     """One call on the current stream of the operands' device."""
     if device.index == torch.cuda.current_device():
         _bind_stream(device)
-        _check(fn(*args))
+        rc = fn(*args)
     else:
         with torch.cuda.device(device):
             _bind_stream(device)
-            _check(fn(*args))
+            rc = fn(*args)
+    if rc != EMU_OK:
+        _check(rc)
 
 
 def _same_gpu(*named):
-    present = [(n, t) for n, t in named if t is not None]
-    _on_gpu(*present)
-    for n, t in present[1:]:
-        if t.device != present[0][1].device:
-            raise ValueError(f"{n} is on {t.device}, {present[0][0]} on {present[0][1].device}")
+    """Every tensor that is given is on the first one's GPU."""
+    first, lead = named[0]
+    device = lead.device
+    for name, t in named:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TypeError(f"{name} must be a GPU tensor")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, {first} on {device}")
 
 
 def _scope(scope: str) -> int:
@@ -345,9 +357,10 @@ def moe_route(logits: torch.Tensor, k: int, scope: str = "chosen") -> Routing:
     T, E = logits.shape
     _same_gpu(("logits", logits))
     dev = logits.device
-    ids, rows, slots = (torch.empty(n, dtype=torch.int32, device=dev) for n in ((T, k), T * k, (T, k)))
-    offsets = torch.empty(E + 1, dtype=torch.int32, device=dev)
-    weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    ids, slots = logits.new_empty((T, k), dtype=torch.int32), logits.new_empty((T, k), dtype=torch.int32)
+    rows = logits.new_empty(T * k, dtype=torch.int32)
+    offsets = logits.new_empty(E + 1, dtype=torch.int32)
+    weights = logits.new_empty((T, k), dtype=torch.float32)
     _launch(lib().emu_moe_route, dev, code, T, E, k, how, logits.data_ptr(), _ld(logits),
             ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
             slots.data_ptr())
@@ -365,7 +378,7 @@ def moe_route_grad(logits, ids, weights, dweights, scope: str = "chosen") -> tor
     _packed(weights, "weights", torch.float32, (T, k))
     _packed(dweights, "dweights", torch.float32, (T, k))
     _same_gpu(("logits", logits), ("ids", ids), ("weights", weights), ("dweights", dweights))
-    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    out = logits.new_empty((T, E))
     _launch(lib().emu_moe_route_grad, logits.device, code, T, E, k, how, logits.data_ptr(),
             _ld(logits), ids.data_ptr(), weights.data_ptr(), dweights.data_ptr(), out.data_ptr(), E)
     return out
@@ -405,8 +418,7 @@ def moe_combine_grad(dY, Z, slots, weights, rows):
         raise ValueError(f"dY must be {T} x {D}, got {tuple(dY.shape)}")
     _packed(rows, "rows", torch.int32, (R,))
     _same_gpu(("Z", Z), ("dY", dY), ("slots", slots), ("weights", weights), ("rows", rows))
-    dZ = torch.empty((R, D), dtype=Z.dtype, device=Z.device)
-    dw = torch.empty((T, k), dtype=torch.float32, device=Z.device)
+    dZ, dw = Z.new_empty((R, D)), torch.empty_like(weights)
     _launch(lib().emu_moe_combine_grad, Z.device, code, T, D, k, R, dY.data_ptr(), _ld(dY),
             Z.data_ptr(), _ld(Z), slots.data_ptr(), weights.data_ptr(), rows.data_ptr(),
             dZ.data_ptr(), max(1, D), dw.data_ptr())
@@ -416,7 +428,7 @@ def moe_combine_grad(dY, Z, slots, weights, rows):
 def _rows_out(Y, R: int, N: int, like, name: str):
     """An output of R rows: allocated when None, else checked to be R x N."""
     if Y is None:
-        return torch.empty((R, N), dtype=like.dtype, device=like.device)
+        return like.new_empty((R, N))
     _float_mat(Y, name, like)
     if tuple(Y.shape) != (R, N):
         raise ValueError(f"{name} must be {R} x {N}, got {tuple(Y.shape)}")
@@ -475,7 +487,7 @@ def grouped_wgrad(X, dY, offsets, dW=None, transb: str = "N", rows=None) -> torc
     _grouping(X, offsets, rows, E, R)
     shape = (E, N, K) if tb else (E, K, N)
     if dW is None:
-        dW = torch.empty(shape, dtype=X.dtype, device=X.device)
+        dW = X.new_empty(shape)
     elif tuple(dW.shape) != shape:
         raise ValueError(f"dW must be {' x '.join(map(str, shape))}, got {tuple(dW.shape)}")
     _, _, _, ldw, stride = _experts(dW, "dW", X.dtype)

@@ -98,15 +98,17 @@ struct Q4Plan {
 template <typename T>
 constexpr int lds_bytes() { return Q4Elem<T>::PLANES == 3 ? 128 * 1024 : 64 * 1024; }
 
-// MT tiles of 16 rows, NT tiles of 16 columns of a wave, groups of G.
-template <typename T, int MT, int NT, int G>
-__global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p) {
+// A tile of MT x 16 rows, NT tiles of 16 columns of a wave, groups of G.  FEW: the
+// tile has at most four rows (MT = 1): row t of the instruction is token t / 4,
+// so that the tokens of a lane's quarter are in one accumulator register instead of
+// four, and the work per group is a quarter.
+template <typename T, int MT, int NT, int G, bool FEW>
+__device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const RowTile &t, char *lds) {
     using C = typename Q4Elem<T>::comp;
     constexpr int PL = Q4Elem<T>::PLANES, U = 4 / NT, GB = BLOCK / G;    // blocks of a set; groups of a block
-    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<T>()];
+    constexpr int REGS = FEW ? 1 : 4, TOKENS = FEW ? 4 : 16 * MT;
+    typedef float sums_t __attribute__((ext_vector_type(REGS)));         // of a lane's tokens
     const int wk = p.wk, wn = WAVES / wk, cols = 16 * NT * wn;
-    const RowTile t = RowTiles(g.offsets, g.E, g.R, 16 * MT, (g.N + cols - 1) / cols).at(blockIdx.x);
-    if (t.e < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int my_n = wave % wn, my_k = wave / wn, h = lane >> 4;
     const int m = (int)(t.end - t.first), K = g.K, N = g.N, col0 = t.col * cols;
@@ -169,11 +171,11 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p)
     float *const sums = reinterpret_cast<float *>(lds + PL * p.tokens * RS);
     const int in_chunk = p.chunk / (wk * U);                        // sets
     const int sets = b_hi > b_lo ? (b_hi - b_lo + wk * U - 1) / (wk * U) : 0;
-    f32x4 y[NT][MT] = {};
+    sums_t y[NT][MT] = {};
     int tok_at[MT];
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
-        const int tok = 16 * a + (lane & 15);
+        const int tok = FEW ? (lane & 15) / 4 : 16 * a + (lane & 15);
         tok_at[a] = (tok < m ? tok : m - 1) * RS + h * 16;
     }
     Set now, next;
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p)
                 // the threads of a group are neighbours, and all of them are here: len is whole groups
 #pragma unroll
                 for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor(sum, d);
-                if (k % G == 0) sums[k / G * (16 * MT) + tok] = sum;
+                if (k % G == 0) sums[k / G * TOKENS + tok] = sum * start;
                 frag<float> v;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[field_place(i)] = x[i];
@@ -229,13 +231,16 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (b * BLOCK + 32 * j >= K) break;
-                const float *const sum = sums + (in * GB + 32 * j / G) * (16 * MT) + 4 * h;
+                const float *const sum = sums + (in * GB + 32 * j / G) * TOKENS + REGS * h;
                 if (32 * j % G == 0) {
 #pragma unroll
                     for (int a = 0; a < MT; ++a) {
-                        const f32x4 v = *reinterpret_cast<const f32x4 *>(sum + 16 * a) * start;
+                        const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
+                        f32x4 c = {};
 #pragma unroll
-                        for (int i = 0; i < NT; ++i) acc[i][a] = v;
+                        for (int r = 0; r < REGS; ++r) c[r] = v[r];
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) acc[i][a] = c;
                     }
                 }
                 frag<C> x[MT][PL];
@@ -258,11 +263,17 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p)
                     for (int i = 0; i < NT; ++i) {
                         const float s = (float)now.s[u][i][32 * j / G];
 #pragma unroll
-                        for (int a = 0; a < MT; ++a) y[i][a] += acc[i][a] * s;
-                        if (g.mins) {
-                            const float o = (float)now.o[u][i][32 * j / G];
+                        for (int a = 0; a < MT; ++a)
 #pragma unroll
-                            for (int a = 0; a < MT; ++a) y[i][a] += *reinterpret_cast<const f32x4 *>(sum + 16 * a) * o;
+                            for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(acc[i][a][r], s, y[i][a][r]);
+                        if (g.mins) {
+                            const float o = (float)now.o[u][i][32 * j / G] * (1.0f / -16.0f);    // of start
+#pragma unroll
+                            for (int a = 0; a < MT; ++a) {
+                                const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
+#pragma unroll
+                                for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(v[r], o, y[i][a][r]);
+                            }
                         }
                     }
                 }
@@ -278,8 +289,8 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p)
 #pragma unroll
         for (int a = 0; a < MT; ++a)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                share[(wave * MT + a) * 256 + (4 * h + r) * 16 + (lane & 15)] = y[i][a][r];
+            for (int r = 0; r < REGS; ++r)
+                share[(wave * MT + a) * 256 + (REGS * h + r) * 16 + (lane & 15)] = y[i][a][r];
         __syncthreads();
         for (int j = threadIdx.x; j < m * 16 * wn; j += 64 * WAVES) {
             const int tok = j / (16 * wn), n = j / 16 % wn, c = j % 16, col = col0 + (n * NT + i) * 16 + c;
@@ -290,6 +301,16 @@ __global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p)
             put(tok, col, v);
         }
     }
+}
+
+template <typename T, int MT, int NT, int G>
+__global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p) {
+    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<T>()];
+    const int cols = 16 * NT * (WAVES / p.wk);
+    const RowTile t = RowTiles(g.offsets, g.E, g.R, 16 * MT, (g.N + cols - 1) / cols).at(blockIdx.x);
+    if (t.e < 0) return;
+    if (MT == 1 && t.end - t.first <= 4) q4_tile<T, MT, NT, G, MT == 1>(g, p, t, lds);
+    else q4_tile<T, MT, NT, G, false>(g, p, t, lds);
 }
 
 // Y = the sum of the parts, in order.
