@@ -136,22 +136,24 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
         s_row[i] = static_cast<const T *>(g.scales) + at * groups;
         m_row[i] = g.mins ? static_cast<const T *>(g.mins) + at * groups : nullptr;
     }
-    // a set: U blocks of the wave's NT columns tiles
+    // a set: U neighbouring blocks of the wave's NT column tiles.  The scales of
+    // all of them are one load: 16 rows of a few bytes cost the address unit as
+    // much as 16 rows of 64.
     struct Set {
         vec<unsigned, 4> w[U][NT];
-        vec<T, GB> s[U][NT], o[U][NT];
+        vec<T, U * GB> s[NT], o[NT];
     };
     auto load_groups = [&](const T *row, int b) {
-        vec<T, GB> v;
-        if (b * GB + GB <= groups) {
-            v = *reinterpret_cast<const vec<T, GB> *>(row + b * GB);
+        vec<T, U * GB> v;
+        if (b * GB + U * GB <= groups) {
+            v = *reinterpret_cast<const vec<T, U * GB> *>(row + b * GB);
         } else {
 #pragma unroll
-            for (int i = 0; i < GB; ++i) v[i] = row[b * GB + i < groups ? b * GB + i : groups - 1];
+            for (int i = 0; i < U * GB; ++i) v[i] = row[b * GB + i < groups ? b * GB + i : groups - 1];
         }
         return v;
     };
-    auto block_of = [&](int set, int u) { return b_lo + (set * U + u) * wk + my_k; };
+    auto block_of = [&](int set, int u) { return b_lo + (set * wk + my_k) * U + u; };
     auto load = [&](Set &x, int set) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -159,11 +161,14 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
             // a run of 32 past the end is read from the row's start and not used
             const int at = b * BLOCK + 32 * h < K ? b * (BLOCK / 2) : -16 * h;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
+            for (int i = 0; i < NT; ++i)
                 x.w[u][i] = __builtin_nontemporal_load(reinterpret_cast<const vec<unsigned, 4> *>(q_row[i] + at));
-                x.s[u][i] = load_groups(s_row[i], b);
-                if (g.mins) x.o[u][i] = load_groups(m_row[i], b);
-            }
+        }
+        const int b = block_of(set, 0);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            x.s[i] = load_groups(s_row[i], b);
+            if (g.mins) x.o[i] = load_groups(m_row[i], b);
         }
     };
     const float start = g.mins ? -16.0f : -24.0f;
@@ -215,11 +220,10 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
             __syncthreads();
         }
         if (set + 1 < sets) load(next, set + 1);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
+        // block u of the set; whole: all of its indices are there
+        auto multiply = [&](int u, auto whole) __attribute__((always_inline)) {
             const int b = block_of(set, u);
-            if (b >= b_hi) break;
-            const int in = (set % in_chunk * U + u) * wk + my_k;       // block of the chunk
+            const int in = (set % in_chunk * wk + my_k) * U + u;       // block of the chunk
             unsigned w[NT][4];
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
@@ -230,7 +234,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
             f32x4 acc[NT][MT];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (b * BLOCK + 32 * j >= K) break;
+                if (!decltype(whole)::value && b * BLOCK + 32 * j >= K) break;
                 const float *const sum = sums + (in * GB + 32 * j / G) * TOKENS + REGS * h;
                 if (32 * j % G == 0) {
 #pragma unroll
@@ -261,13 +265,13 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
                 if ((32 * j + 32) % G == 0) {
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
-                        const float s = (float)now.s[u][i][32 * j / G];
+                        const float s = (float)now.s[i][u * GB + 32 * j / G];
 #pragma unroll
                         for (int a = 0; a < MT; ++a)
 #pragma unroll
                             for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(acc[i][a][r], s, y[i][a][r]);
                         if (g.mins) {
-                            const float o = (float)now.o[u][i][32 * j / G] * (1.0f / -16.0f);    // of start
+                            const float o = (float)now.o[i][u * GB + 32 * j / G] * (1.0f / -16.0f);    // of start
 #pragma unroll
                             for (int a = 0; a < MT; ++a) {
                                 const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
@@ -278,6 +282,14 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
                     }
                 }
             }
+        };
+        if (block_of(set, U - 1) < b_hi && (block_of(set, U - 1) + 1) * BLOCK <= K) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) multiply(u, std::true_type{});
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (block_of(set, u) < b_hi) multiply(u, std::false_type{});
         }
         now = next;
     }
