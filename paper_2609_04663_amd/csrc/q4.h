@@ -89,59 +89,131 @@ __device__ __forceinline__ void exchange_quarters(unsigned (&d)[4]) {
 // What a launch fixes for all of its workgroups.
 struct Q4Plan {
     int wk;                         // waves along the reduction, of 8; the others are along the columns
-    int chunk;                      // blocks of 128 indices that x is staged for at a time
-    int tokens;                     // most rows of a tile
+    int passes;                     // column tiles of a workgroup, one after the other
     int splits;                     // workgroups along the reduction
     float *part;                    // splits x R x N sums where splits > 1
 };
 
-template <typename T>
-constexpr int lds_bytes() { return Q4Elem<T>::PLANES == 3 ? 128 * 1024 : 64 * 1024; }
+// LDS: x as components, 16 bytes longer than its indices per token so that the
+// tokens of a read lie in different banks; its sums per group; and 1 KB for each
+// wave and tile of 16 rows, where the waves along the reduction add up.
+template <typename T, int MT>
+constexpr int lds_bytes() { return (Q4Elem<T>::PLANES == 3 ? 144 : (MT == 1 ? 64 : 128)) * 1024; }
+template <typename T, int MT>
+constexpr int share_at() { return lds_bytes<T, MT>() - WAVES * MT * 1024; }
+// blocks of x of `tokens` tokens (sums of `slots` tokens) that fit
+template <typename T, int MT>
+__host__ __device__ constexpr int blocks_that_fit(int tokens, int slots, int group) {
+    const int each = Q4Elem<T>::PLANES * tokens * 2 * BLOCK + slots * 4 * (BLOCK / group);
+    return (share_at<T, MT>() - 16 * Q4Elem<T>::PLANES * tokens) / each;
+}
 
-// A tile of MT x 16 rows, NT tiles of 16 columns of a wave, groups of G.  FEW: the
-// tile has at most four rows (MT = 1): row t of the instruction is token t / 4,
-// so that the tokens of a lane's quarter are in one accumulator register instead of
-// four, and the work per group is a quarter.
-template <typename T, int MT, int NT, int G, bool FEW>
+// A tile of MT x 16 rows, NT tiles of 16 columns of a wave, sets of U blocks of
+// 128 indices, groups of G.  FEW: the tile has at most four rows (MT = 1): row t
+// of the instruction is token t / 4, so that the tokens of a lane's quarter are in
+// one accumulator register instead of four, and the work per group is a quarter.
+template <typename T, int MT, int NT, int U, int G, bool FEW>
 __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const RowTile &t, char *lds) {
     using C = typename Q4Elem<T>::comp;
-    constexpr int PL = Q4Elem<T>::PLANES, U = 4 / NT, GB = BLOCK / G;    // blocks of a set; groups of a block
+    constexpr int PL = Q4Elem<T>::PLANES, GB = BLOCK / G;                // groups of a block
     constexpr int REGS = FEW ? 1 : 4, TOKENS = FEW ? 4 : 16 * MT;
+    constexpr int THREADS = 64 * WAVES;
+    static_assert(blocks_that_fit<T, MT>(16 * MT, 16 * MT, 32) >= U, "a set's blocks");
     typedef float sums_t __attribute__((ext_vector_type(REGS)));         // of a lane's tokens
     const int wk = p.wk, wn = WAVES / wk, cols = 16 * NT * wn;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int my_n = wave % wn, my_k = wave / wn, h = lane >> 4;
-    const int m = (int)(t.end - t.first), K = g.K, N = g.N, col0 = t.col * cols;
+    const int m = (int)(t.end - t.first), K = g.K, N = g.N;
+    const int col0 = t.col * cols * p.passes;
     float *const part = p.part ? p.part + (int64_t)blockIdx.y * g.R * N : nullptr;
     T *const Y = static_cast<T *>(g.Y);
     auto put = [&](int tok, int col, float v) {
         if (part) part[(t.first + tok) * N + col] = v;
         else Y[(t.first + tok) * g.ldy + col] = (T)v;
     };
+    const int left = (N - col0 + cols - 1) / cols, passes = left < p.passes ? left : p.passes;
     if (t.e == g.E) {                                 // rows of no expert
-        for (int i = threadIdx.x; i < m * cols; i += 64 * WAVES)
-            if (col0 + i % cols < N) put(i / cols, col0 + i % cols, 0.0f);
+        for (int i = threadIdx.x; i < m * cols * passes; i += THREADS) {
+            const int c = col0 + i % (cols * passes);
+            if (c < N) put(i / (cols * passes), c, 0.0f);
+        }
         return;
     }
     const int groups = K / G, blocks = (K + BLOCK - 1) / BLOCK;
     const int per = (blocks + p.splits - 1) / p.splits;
     const int b_lo = blockIdx.y * per, b_hi = b_lo + per < blocks ? b_lo + per : blocks;
-    const uint8_t *q_row[NT];
-    const T *s_row[NT], *m_row[NT];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        const int n = col0 + (my_n * NT + i) * 16 + (lane & 15);
-        const int64_t at = (int64_t)t.e * N + (n < N ? n : N - 1);
-        q_row[i] = g.Q + at * (K / 2) + 16 * h;
-        s_row[i] = static_cast<const T *>(g.scales) + at * groups;
-        m_row[i] = g.mins ? static_cast<const T *>(g.mins) + at * groups : nullptr;
+    const int step = wk * U, need = b_hi > b_lo ? (b_hi - b_lo + step - 1) / step * step : 0;
+    const int sets = need / step;
+
+    // x: all of it at once, staged for every pass, or a chunk at a time
+    const int fit = blocks_that_fit<T, MT>(m, TOKENS, G) / step * step;
+    const bool once = need <= fit;
+    const int chunk = once ? need : fit, in_chunk = chunk > 0 ? chunk / step : 1;   // blocks; sets
+    const int RS = chunk * BLOCK * 2 + 16, sums_at = PL * m * RS;
+    const float start = g.mins ? -16.0f : -24.0f;
+    // the row of each token, looked up once
+    __shared__ int row_of[16 * MT];
+    if ((int)threadIdx.x < m) {
+        const int64_t r = t.first + threadIdx.x, at = g.rows ? g.rows[r] : r;
+        row_of[threadIdx.x] = at >= 0 && at < g.xrows ? (int)at : -1;
     }
+    typedef vec<T, 8> run_t;
+    auto fetch = [&](int u, int runs, int c0) {
+        const int at = row_of[u / runs];
+        run_t v = run_t{};
+        if (at >= 0)
+            v = *reinterpret_cast<const run_t *>(static_cast<const T *>(g.X) + at * g.ldx + c0 + u % runs * 8);
+        return v;
+    };
+    // run u (eight indices of a token) into the buffer; the threads of a group are
+    // neighbours, and all of them are here: a chunk is whole groups
+    auto deposit = [&](char *buf, int u, int runs, const run_t &v) {
+        const int tok = u / runs, k = u % runs * 8;
+        frag<float> x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
+        float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+#pragma unroll
+        for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor(sum, d);
+        if (k % G == 0) reinterpret_cast<float *>(buf + sums_at)[k / G * TOKENS + tok] = sum * start;
+        frag<float> f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[field_place(i)] = x[i];
+#pragma unroll
+        for (int c = 0; c < PL; ++c) {
+            const frag<C> w = __builtin_convertvector(f, frag<C>);
+            *reinterpret_cast<frag<C> *>(buf + (c * m + tok) * RS + k * 2) = w;
+            if (c + 1 < PL) f = f - __builtin_convertvector(w, frag<float>);
+        }
+    };
+    // indices of the chunk that starts with block b
+    auto chunk_runs = [&](int b) {
+        const int hi = b_hi * BLOCK < K ? b_hi * BLOCK : K, len = hi - b * BLOCK;
+        return (len < chunk * BLOCK ? len : chunk * BLOCK) / 8;
+    };
+    auto stage = [&](int b) {
+        const int runs = chunk_runs(b);
+        for (int u = threadIdx.x; u < m * runs; u += THREADS) deposit(lds, u, runs, fetch(u, runs, b * BLOCK));
+    };
+
     // a set: U neighbouring blocks of the wave's NT column tiles.  The scales of
     // all of them are one load: 16 rows of a few bytes cost the address unit as
     // much as 16 rows of 64.
     struct Set {
         vec<unsigned, 4> w[U][NT];
         vec<T, U * GB> s[NT], o[NT];
+    };
+    const uint8_t *q_row[NT];
+    const T *s_row[NT], *m_row[NT];
+    auto point = [&](int pass) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int n = col0 + pass * cols + (my_n * NT + i) * 16 + (lane & 15);
+            const int64_t at = (int64_t)t.e * N + (n < N ? n : N - 1);
+            q_row[i] = g.Q + at * (K / 2) + 16 * h;
+            s_row[i] = static_cast<const T *>(g.scales) + at * groups;
+            m_row[i] = g.mins ? static_cast<const T *>(g.mins) + at * groups : nullptr;
+        }
     };
     auto load_groups = [&](const T *row, int b) {
         vec<T, U * GB> v;
@@ -171,11 +243,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
             if (g.mins) x.o[i] = load_groups(m_row[i], b);
         }
     };
-    const float start = g.mins ? -16.0f : -24.0f;
-    const int RS = p.chunk * BLOCK * 2 + 16;
-    float *const sums = reinterpret_cast<float *>(lds + PL * p.tokens * RS);
-    const int in_chunk = p.chunk / (wk * U);                        // sets
-    const int sets = b_hi > b_lo ? (b_hi - b_lo + wk * U - 1) / (wk * U) : 0;
+
     sums_t y[NT][MT] = {};
     int tok_at[MT];
 #pragma unroll
@@ -184,145 +252,147 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
         tok_at[a] = (tok < m ? tok : m - 1) * RS + h * 16;
     }
     Set now, next;
+    point(0);
     if (sets > 0) load(now, 0);
-    for (int set = 0; set < sets; ++set) {
-        if (set % in_chunk == 0) {
-            const int c0 = (b_lo + set * U * wk) * BLOCK;
-            const int len = K - c0 < p.chunk * BLOCK ? K - c0 : p.chunk * BLOCK;
-            const int runs = len / 8;
-            if (set > 0) __syncthreads();
-            // stage x: a thread takes eight indices of a token
-            for (int u = threadIdx.x; u < m * runs; u += 64 * WAVES) {
-                const int tok = u / runs, k = u % runs * 8;
-                const int64_t r = t.first + tok, at = g.rows ? g.rows[r] : r;
-                frag<float> x = frag<float>{};
-                if (at >= 0 && at < g.xrows) {
-                    const vec<T, 8> v = *reinterpret_cast<const vec<T, 8> *>(
-                        static_cast<const T *>(g.X) + at * g.ldx + c0 + k);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-                }
-                float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-                // the threads of a group are neighbours, and all of them are here: len is whole groups
-#pragma unroll
-                for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor(sum, d);
-                if (k % G == 0) sums[k / G * TOKENS + tok] = sum * start;
-                frag<float> v;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[field_place(i)] = x[i];
-#pragma unroll
-                for (int c = 0; c < PL; ++c) {
-                    const frag<C> f = __builtin_convertvector(v, frag<C>);
-                    *reinterpret_cast<frag<C> *>(lds + (c * p.tokens + tok) * RS + k * 2) = f;
-                    if (c + 1 < PL) v = v - __builtin_convertvector(f, frag<float>);
-                }
+    __syncthreads();                                  // row_of
+    char *const buf = lds;
+    // the sets of all passes; without any (K = 0), the passes alone
+    int pass = 0, set = 0;
+    do {
+        if (sets > 0) {
+            if (set % in_chunk == 0 && (!once || pass == 0)) {
+                if (pass + set > 0) __syncthreads();  // every wave is done with the chunk before
+                stage(b_lo + set * step);
+                __syncthreads();
             }
-            __syncthreads();
-        }
-        if (set + 1 < sets) load(next, set + 1);
-        // block u of the set; whole: all of its indices are there
-        auto multiply = [&](int u, auto whole) __attribute__((always_inline)) {
-            const int b = block_of(set, u);
-            const int in = (set % in_chunk * wk + my_k) * U + u;       // block of the chunk
-            unsigned w[NT][4];
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w[i][j] = now.w[u][i][j];
-                exchange_quarters(w[i]);
-            }
-            f32x4 acc[NT][MT];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (!decltype(whole)::value && b * BLOCK + 32 * j >= K) break;
-                const float *const sum = sums + (in * GB + 32 * j / G) * TOKENS + REGS * h;
-                if (32 * j % G == 0) {
-#pragma unroll
-                    for (int a = 0; a < MT; ++a) {
-                        const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
-                        f32x4 c = {};
-#pragma unroll
-                        for (int r = 0; r < REGS; ++r) c[r] = v[r];
-#pragma unroll
-                        for (int i = 0; i < NT; ++i) acc[i][a] = c;
-                    }
-                }
-                frag<C> x[MT][PL];
-#pragma unroll
-                for (int a = 0; a < MT; ++a)
-#pragma unroll
-                    for (int c = 0; c < PL; ++c)
-                        x[a][c] = *reinterpret_cast<const frag<C> *>(lds + tok_at[a] + c * p.tokens * RS +
-                                                                     (in * BLOCK + 32 * j) * 2);
+            // the set after this one, or the next pass's first (after the last, that again)
+            if (set + 1 == sets && pass + 1 < passes) point(pass + 1);
+            load(next, set + 1 < sets ? set + 1 : (pass + 1 < passes ? 0 : set));
+            const float *const sums = reinterpret_cast<const float *>(buf + sums_at);
+            // block u of the set; whole: all of its indices are there
+            auto multiply = [&](int u, auto whole) __attribute__((always_inline)) {
+                const int b = block_of(set, u);
+                const int in = (set % in_chunk * wk + my_k) * U + u;     // block of the chunk
+                unsigned w[NT][4];
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
-                    const frag<C> wf = sixteen_plus<C>(w[i][j]);
 #pragma unroll
-                    for (int c = PL - 1; c >= 0; --c)
-#pragma unroll
-                        for (int a = 0; a < MT; ++a) acc[i][a] = mfma16(x[a][c], wf, acc[i][a]);
+                    for (int j = 0; j < 4; ++j) w[i][j] = now.w[u][i][j];
+                    exchange_quarters(w[i]);
                 }
-                if ((32 * j + 32) % G == 0) {
+                f32x4 acc[NT][MT];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!decltype(whole)::value && b * BLOCK + 32 * j >= K) break;
+                    const float *const sum = sums + (in * GB + 32 * j / G) * TOKENS + REGS * h;
+                    if (32 * j % G == 0) {
+#pragma unroll
+                        for (int a = 0; a < MT; ++a) {
+                            const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
+                            f32x4 c = {};
+#pragma unroll
+                            for (int r = 0; r < REGS; ++r) c[r] = v[r];
+#pragma unroll
+                            for (int i = 0; i < NT; ++i) acc[i][a] = c;
+                        }
+                    }
+                    frag<C> x[MT][PL];
+#pragma unroll
+                    for (int a = 0; a < MT; ++a)
+#pragma unroll
+                        for (int c = 0; c < PL; ++c)
+                            x[a][c] = *reinterpret_cast<const frag<C> *>(buf + tok_at[a] + c * m * RS +
+                                                                         (in * BLOCK + 32 * j) * 2);
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
-                        const float s = (float)now.s[i][u * GB + 32 * j / G];
+                        const frag<C> wf = sixteen_plus<C>(w[i][j]);
 #pragma unroll
-                        for (int a = 0; a < MT; ++a)
+                        for (int c = PL - 1; c >= 0; --c)
 #pragma unroll
-                            for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(acc[i][a][r], s, y[i][a][r]);
-                        if (g.mins) {
-                            const float o = (float)now.o[i][u * GB + 32 * j / G] * (1.0f / -16.0f);    // of start
+                            for (int a = 0; a < MT; ++a) acc[i][a] = mfma16(x[a][c], wf, acc[i][a]);
+                    }
+                    // reads of the next run do not start before this point: no registers for more
+                    if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+                    if ((32 * j + 32) % G == 0) {
 #pragma unroll
-                            for (int a = 0; a < MT; ++a) {
-                                const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
+                        for (int i = 0; i < NT; ++i) {
+                            const float s = (float)now.s[i][u * GB + 32 * j / G];
 #pragma unroll
-                                for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(v[r], o, y[i][a][r]);
+                            for (int a = 0; a < MT; ++a)
+#pragma unroll
+                                for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(acc[i][a][r], s, y[i][a][r]);
+                            if (g.mins) {
+                                const float o = (float)now.o[i][u * GB + 32 * j / G] * (1.0f / -16.0f);  // of start
+#pragma unroll
+                                for (int a = 0; a < MT; ++a) {
+                                    const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
+#pragma unroll
+                                    for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(v[r], o, y[i][a][r]);
+                                }
                             }
                         }
                     }
                 }
+            };
+            if (block_of(set, U - 1) < b_hi && (block_of(set, U - 1) + 1) * BLOCK <= K) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) multiply(u, std::true_type{});
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (block_of(set, u) < b_hi) multiply(u, std::false_type{});
             }
-        };
-        if (block_of(set, U - 1) < b_hi && (block_of(set, U - 1) + 1) * BLOCK <= K) {
-#pragma unroll
-            for (int u = 0; u < U; ++u) multiply(u, std::true_type{});
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (block_of(set, u) < b_hi) multiply(u, std::false_type{});
+            now = next;
+            if (++set < sets) continue;
+            set = 0;
         }
-        now = next;
-    }
-    // the sums of the waves along the reduction, in order
-    float *const share = reinterpret_cast<float *>(lds);
+        // the pass's results: the lanes' own, or the sums of the waves along the reduction, in order
+        const int c0 = col0 + pass * cols;
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        __syncthreads();
+        for (int i = 0; i < NT; ++i) {
+            if (wk == 1) {
+                const int col = c0 + (my_n * NT + i) * 16 + (lane & 15);
 #pragma unroll
-        for (int a = 0; a < MT; ++a)
+                for (int a = 0; a < MT; ++a)
 #pragma unroll
-            for (int r = 0; r < REGS; ++r)
-                share[(wave * MT + a) * 256 + (REGS * h + r) * 16 + (lane & 15)] = y[i][a][r];
-        __syncthreads();
-        for (int j = threadIdx.x; j < m * 16 * wn; j += 64 * WAVES) {
-            const int tok = j / (16 * wn), n = j / 16 % wn, c = j % 16, col = col0 + (n * NT + i) * 16 + c;
-            if (col >= N) continue;
-            float v = 0.0f;
-            for (int w = 0; w < wk; ++w)
-                v += share[((w * wn + n) * MT + tok / 16) * 256 + tok % 16 * 16 + c];
-            put(tok, col, v);
+                    for (int r = 0; r < REGS; ++r) {
+                        const int tok = 16 * a + REGS * h + r;
+                        if (tok < m && col < N) put(tok, col, y[i][a][r]);
+                    }
+            } else {
+                float *const share = reinterpret_cast<float *>(lds + share_at<T, MT>());
+                if (pass + i > 0) __syncthreads();
+#pragma unroll
+                for (int a = 0; a < MT; ++a)
+#pragma unroll
+                    for (int r = 0; r < REGS; ++r)
+                        share[(wave * MT + a) * 256 + (REGS * h + r) * 16 + (lane & 15)] = y[i][a][r];
+                __syncthreads();
+                for (int j = threadIdx.x; j < m * 16 * wn; j += THREADS) {
+                    const int tok = j / (16 * wn), n = j / 16 % wn, c = j % 16, col = c0 + (n * NT + i) * 16 + c;
+                    if (col >= N) continue;
+                    float v = 0.0f;
+                    for (int w = 0; w < wk; ++w)
+                        v += share[((w * wn + n) * MT + tok / 16) * 256 + tok % 16 * 16 + c];
+                    put(tok, col, v);
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < MT; ++a) y[i][a] = sums_t{};
         }
-    }
+        ++pass;
+    } while (pass < passes);
 }
 
-template <typename T, int MT, int NT, int G>
-__global__ __launch_bounds__(64 * WAVES) void q4_gemm_kernel(Q4Gemm g, Q4Plan p) {
-    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<T>()];
-    const int cols = 16 * NT * (WAVES / p.wk);
+template <typename T, int MT, int NT, int U, int G>
+__global__ __launch_bounds__(64 * WAVES, MT == 1 && Q4Elem<T>::PLANES == 1 ? 4 : 2) void q4_gemm_kernel(Q4Gemm g,
+                                                                                                         Q4Plan p) {
+    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<T, MT>()];
+    const int cols = 16 * NT * (WAVES / p.wk) * p.passes;
     const RowTile t = RowTiles(g.offsets, g.E, g.R, 16 * MT, (g.N + cols - 1) / cols).at(blockIdx.x);
     if (t.e < 0) return;
-    if (MT == 1 && t.end - t.first <= 4) q4_tile<T, MT, NT, G, MT == 1>(g, p, t, lds);
-    else q4_tile<T, MT, NT, G, false>(g, p, t, lds);
+    if (MT == 1 && t.end - t.first <= 4) q4_tile<T, MT, NT, U, G, MT == 1>(g, p, t, lds);
+    else q4_tile<T, MT, NT, U, G, false>(g, p, t, lds);
 }
 
 // Y = the sum of the parts, in order.
@@ -347,30 +417,24 @@ int64_t likely_tiles(const Q4Gemm &g, int rows) {
     return full > reached ? full : reached;
 }
 
-template <typename T, int MT, int NT>
+template <typename T, int MT, int NT, int U>
 Q4Plan plan_q4(const Q4Gemm &g) {
-    constexpr int U = 4 / NT;
     Q4Plan p = {};
-    p.tokens = g.R < 16 * MT ? (int)g.R : 16 * MT;
-    const int blocks = (g.K + BLOCK - 1) / BLOCK;
-    const int each = Q4Elem<T>::PLANES * p.tokens * 2 * BLOCK + 16 * MT * 4 * (BLOCK / g.group);
-    const int fit = (lds_bytes<T>() - 16 * Q4Elem<T>::PLANES * p.tokens) / each;
-    // waves along the columns, as long as there are WAVES_MIN waves for the chip
-    constexpr int64_t WAVES_MIN = 16 * 256;
+    const int tokens = g.R < 16 * MT ? (int)g.R : 16 * MT;
+    const int blocks = (g.K + BLOCK - 1) / BLOCK, fit = blocks_that_fit<T, MT>(tokens, 16 * MT, g.group);
+    const int64_t rows = likely_tiles(g, 16 * MT);
+    auto col_tiles = [&](int wk) { return (g.N + 16 * NT * (WAVES / wk) - 1) / (16 * NT * (WAVES / wk)); };
+    // waves along the columns, as long as there are 16 waves for each CU
     p.wk = WAVES;
-    while (p.wk > 1 && (p.wk * U > fit ||
-                        likely_tiles(g, 16 * MT) * ((g.N + 16 * NT * 2 * (WAVES / p.wk) - 1) /
-                                                    (16 * NT * 2 * (WAVES / p.wk))) * WAVES >= WAVES_MIN))
-        p.wk /= 2;
-    const int step = p.wk * U, need = (blocks + step - 1) / step * step;
-    p.chunk = fit / step * step;
-    if (p.chunk > need) p.chunk = need;
-    if (p.chunk < step) p.chunk = step;               // K = 0
+    while (p.wk > 1 && (p.wk * U > fit || rows * col_tiles(p.wk / 2) * WAVES >= 16 * 256)) p.wk /= 2;
     // few workgroups with long reductions: more along the reduction
-    const int cols = 16 * NT * (WAVES / p.wk);
-    const int64_t tiles = likely_tiles(g, 16 * MT) * ((g.N + cols - 1) / cols);
+    const int64_t tiles = rows * col_tiles(p.wk);
     p.splits = 1;
-    while (p.splits < 16 && tiles * p.splits * 2 <= 256 && blocks / (p.splits * 2) >= 4 * step) p.splits *= 2;
+    while (p.splits < 16 && tiles * p.splits * 2 <= 256 && blocks / (p.splits * 2) >= 4 * p.wk * U) p.splits *= 2;
+    // more workgroups than run at a time: column tiles one after the other in
+    // each, so that x is staged once for them and the loads never pause
+    p.passes = 1;
+    while (p.passes < 16 && tiles >= 512 * 2 * p.passes) p.passes *= 2;
     return p;
 }
 
@@ -379,9 +443,9 @@ Q4Plan plan_q4(const Q4Gemm &g) {
 template <typename T>
 hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
     hipError_t e = hipSuccess;
-    auto run = [&](auto mt, auto nt, auto group) {
-        constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
-        Q4Plan p = plan_q4<T, MT, NT>(g);
+    auto run = [&](auto mt, auto nt, auto set, auto group) {
+        constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value, U = decltype(set)::value;
+        Q4Plan p = plan_q4<T, MT, NT, U>(g);
         if (p.splits > 1) {
             char *w = nullptr;
             if (api_workspace(sizeof(float) * p.splits * g.R * g.N, &w) != EMU_OK) {
@@ -390,9 +454,9 @@ hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
             }
             p.part = reinterpret_cast<float *>(w);
         }
-        const int cols = 16 * NT * (WAVES / p.wk);
+        const int cols = 16 * NT * (WAVES / p.wk) * p.passes;
         const int64_t tiles = row_blocks_bound(g.R, g.E, 16 * MT) * ((g.N + cols - 1) / cols);
-        q4_gemm_kernel<T, MT, NT, decltype(group)::value><<<dim3((unsigned)tiles, p.splits), 64 * WAVES, 0, s>>>(g, p);
+        q4_gemm_kernel<T, MT, NT, U, decltype(group)::value><<<dim3((unsigned)tiles, p.splits), 64 * WAVES, 0, s>>>(g, p);
         e = hipGetLastError();
         if (e == hipSuccess && p.splits > 1) {
             q4_join_kernel<T><<<(unsigned)((g.R * g.N + 255) / 256), 256, 0, s>>>(p.part, p.splits, g.R, g.N,
@@ -406,10 +470,12 @@ hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
         const integral_constant<int, 2> two;
         const integral_constant<int, 3> three;
         const integral_constant<int, 4> four;
-        if (g.R <= 16 * (int64_t)g.E) run(one, one, group);
-        else if (g.R <= 32 * (int64_t)g.E) run(two, four, group);
-        else if (g.R <= 48 * (int64_t)g.E) run(three, integral_constant<int, Q4Elem<T>::PLANES == 3 ? 2 : 4>{}, group);
-        else run(four, two, group);
+        // a wave has 4 KB of weights in flight
+        constexpr bool wide = Q4Elem<T>::PLANES == 3;
+        if (g.R <= 16 * (int64_t)g.E) run(one, one, four, group);
+        else if (g.R <= 32 * (int64_t)g.E) run(two, four, one, group);
+        else if (g.R <= 48 * (int64_t)g.E) run(three, integral_constant<int, wide ? 2 : 4>{}, integral_constant<int, wide ? 2 : 1>{}, group);
+        else run(four, two, two, group);
     };
     if (g.group == 32) rows(std::integral_constant<int, 32>{});
     else if (g.group == 64) rows(std::integral_constant<int, 64>{});
