@@ -151,4 +151,23 @@ struct RowTiles {
     }
 };
 
+// One 1 KB copy: lane l moves 16 bytes from its own source to dst + 16 l (dst
+// and base uniform over the wave).  Inline asm, which has no output register:
+// the compiler takes a transposing LDS read to depend on every such copy in
+// flight and would wait for the one just issued before each read.  The kernels
+// wait for them themselves (s_waitcnt vmcnt before a barrier).  The s_nop is
+// the wait state between a write of m0 (which the compiler keeps nothing in) and
+// its use by the copy.
+__device__ __forceinline__ unsigned lds_address(char *p) {
+    return (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)p;
+}
+__device__ __forceinline__ void copy_lanes(const char *base, unsigned offset, char *dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                 :: "s"(lds_address(dst)), "v"(offset), "s"(base) : "memory");
+}
+__device__ __forceinline__ void copy_lanes(const char *src, char *dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(lds_address(dst)), "v"(src) : "memory");
+}
+
 }  // namespace emu

@@ -1,21 +1,27 @@
-// Products of a few rows with matrices in 4 bits, Y[r] = X[r] W[e(r)]^T, and the
-// packing of those matrices.
+// Products of a few rows with matrices in 4 bits, Y[r] = X[r] W[e(r)]^T.
 //
 // Arithmetic.  An integer q of a weight becomes the exact 16 + q in the matrix
-// instruction's type with one shift and one and-or for two weights (its four
-// bits below the exponent of 16), so a group's sum is sum (16 + q) x in FP32,
-// and s (q - 8) summed over a group is s times that sum started at -24 sum x
-// (-16 sum x with offsets, plus m sum x).  The sums of x per group are made once
-// where x is staged.  FP32 rows are three BF16 components (Eq. fp32split) and
-// three products with the same weights.  No weight is rounded.
+// instruction's type with a shift, an and, and an or for two weights (its four
+// bits below the exponent of 16), so a group's sum is sum (16 + q) x in FP32, and
+// s (q - 8) summed over the group is s times (that sum - 24 sum x); with offsets
+// s times (that sum - 16 sum x) plus m sum x.  FP32 rows are three BF16 components
+// (Eq. fp32split) and three products with the same weights.  No weight is rounded.
 //
 // Shape.  v_mfma 16 x 16 x 32 with tokens as rows and weight rows as columns: a
 // lane loads 16 bytes, 32 indices of one weight row; four lanes of a row hold
 // 128, and a 4 x 4 exchange between them (two v_permlane32_swap, two
 // v_permlane16_swap) makes each instruction span one run of 32, so that groups
-// of 32 can be scaled.  The waves of a workgroup share the reduction (and
-// the columns, where x leaves room in LDS for few indices only) and add up
-// their sums in LDS at the end.
+// of 32 can be scaled.  x lies in LDS, the 16-byte units of token t permuted by
+// t % 16, so that the 16 tokens of a read touch every bank once.  Two forms:
+//   prepared (FP32, and tiles of at most four rows): the components in the order
+//     of the weights' fields, with the sums of each group, made as x is staged;
+//   raw (more rows of 16 bits): copied as it is by global_load_lds, a chunk ahead
+//     in a second buffer where it does not fit at once; a fragment is put into the
+//     fields' order after it is read, and one more matrix instruction with ones
+//     gives the sums.  16 rows of 16384 x 16384: 63 us, prepared 84; one row of
+//     64 matrices of 4096 x 4096: 136 us, prepared 118.
+// The waves of a workgroup share the reduction (and the columns, where x leaves
+// room for few indices only) and add up their sums in LDS at the end.
 #pragma once
 
 #include "api_state.h"
@@ -66,8 +72,17 @@ __device__ __forceinline__ frag<C> sixteen_plus(unsigned w) {
     }
     return __builtin_bit_cast(frag<C>, r);
 }
-// where element i of eight consecutive ones goes to match it
-__device__ __forceinline__ constexpr int field_place(int i) { return i % 4 * 2 + i / 4; }
+// Eight consecutive entries of x in the order that matches it.
+template <typename C>
+__device__ __forceinline__ frag<C> to_fields(frag<C> x) {
+    const u32x4 r = __builtin_bit_cast(u32x4, x);
+    u32x4 f;
+    f[0] = __builtin_amdgcn_perm(r[2], r[0], 0x05040100u);      // entries 0, 4
+    f[1] = __builtin_amdgcn_perm(r[2], r[0], 0x07060302u);      // 1, 5
+    f[2] = __builtin_amdgcn_perm(r[3], r[1], 0x05040100u);      // 2, 6
+    f[3] = __builtin_amdgcn_perm(r[3], r[1], 0x07060302u);      // 3, 7
+    return __builtin_bit_cast(frag<C>, f);
+}
 
 // Lane quarter h of register i gets quarter i's register h.
 __device__ __forceinline__ void exchange_quarters(unsigned (&d)[4]) {
@@ -92,21 +107,33 @@ struct Q4Plan {
     int passes;                     // column tiles of a workgroup, one after the other
     int splits;                     // workgroups along the reduction
     float *part;                    // splits x R x N sums where splits > 1
+    bool copies;                    // X is 16-byte aligned
 };
 
-// LDS: x as components, 16 bytes longer than its indices per token so that the
-// tokens of a read lie in different banks; its sums per group; and 1 KB for each
-// wave and tile of 16 rows, where the waves along the reduction add up.
+// LDS: x, one buffer or two (prepared: with its sums per group); and 1 KB for
+// each wave and tile of 16 rows, where the waves along the reduction add up.
 template <typename T, int MT>
-constexpr int lds_bytes() { return (Q4Elem<T>::PLANES == 3 ? 144 : (MT == 1 ? 64 : 128)) * 1024; }
+constexpr int lds_bytes() { return (Q4Elem<T>::PLANES == 3 ? 152 : (MT == 1 ? 72 : 128)) * 1024; }
 template <typename T, int MT>
 constexpr int share_at() { return lds_bytes<T, MT>() - WAVES * MT * 1024; }
-// blocks of x of `tokens` tokens (sums of `slots` tokens) that fit
-template <typename T, int MT>
-__host__ __device__ constexpr int blocks_that_fit(int tokens, int slots, int group) {
-    const int each = Q4Elem<T>::PLANES * tokens * 2 * BLOCK + slots * 4 * (BLOCK / group);
-    return (share_at<T, MT>() - 16 * Q4Elem<T>::PLANES * tokens) / each;
+// bytes of a buffer for `chunk` blocks of 128 indices of m tokens: components (the
+// copies write whole KB), and sums for `slots` tokens
+template <typename T>
+__host__ __device__ constexpr int sums_at(int m, int chunk) {
+    return (Q4Elem<T>::PLANES * m * chunk * 256 + 1023) / 1024 * 1024;
 }
+template <typename T>
+__host__ __device__ constexpr int buffer_bytes(int m, int slots, int group, int chunk) {
+    return sums_at<T>(m, chunk) + chunk * (BLOCK / group) * slots * 4;
+}
+// blocks that a buffer of the given size holds
+template <typename T>
+__host__ __device__ constexpr int blocks_that_fit(int m, int slots, int group, int bytes) {
+    return (bytes - 1024) / (Q4Elem<T>::PLANES * m * 256 + BLOCK / group * slots * 4);
+}
+
+// Sixteen zero bytes: rows outside.
+__device__ __attribute__((aligned(16))) float g_zero16[4];
 
 // A tile of MT x 16 rows, NT tiles of 16 columns of a wave, sets of U blocks of
 // 128 indices, groups of G.  FEW: the tile has at most four rows (MT = 1): row t
@@ -117,8 +144,10 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     using C = typename Q4Elem<T>::comp;
     constexpr int PL = Q4Elem<T>::PLANES, GB = BLOCK / G;                // groups of a block
     constexpr int REGS = FEW ? 1 : 4, TOKENS = FEW ? 4 : 16 * MT;
+    constexpr bool RAW = PL == 1 && !FEW;
+    constexpr int SLOTS = RAW ? 0 : TOKENS;                              // sums of a group
     constexpr int THREADS = 64 * WAVES;
-    static_assert(blocks_that_fit<T, MT>(16 * MT, 16 * MT, 32) >= U, "a set's blocks");
+    static_assert(blocks_that_fit<T>(16 * MT, 16 * MT, 32, share_at<T, MT>()) >= U, "a set's blocks");
     typedef float sums_t __attribute__((ext_vector_type(REGS)));         // of a lane's tokens
     const int wk = p.wk, wn = WAVES / wk, cols = 16 * NT * wn;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -142,58 +171,67 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     const int groups = K / G, blocks = (K + BLOCK - 1) / BLOCK;
     const int per = (blocks + p.splits - 1) / p.splits;
     const int b_lo = blockIdx.y * per, b_hi = b_lo + per < blocks ? b_lo + per : blocks;
-    const int step = wk * U, need = b_hi > b_lo ? (b_hi - b_lo + step - 1) / step * step : 0;
-    const int sets = need / step;
+    const int step = wk * U, sets = b_hi > b_lo ? (b_hi - b_lo + step - 1) / step : 0;
 
-    // x: all of it at once, staged for every pass, or a chunk at a time
-    const int fit = blocks_that_fit<T, MT>(m, TOKENS, G) / step * step;
-    const bool once = need <= fit;
-    const int chunk = once ? need : fit, in_chunk = chunk > 0 ? chunk / step : 1;   // blocks; sets
-    const int RS = chunk * BLOCK * 2 + 16, sums_at = PL * m * RS;
+    // x: all of it at once, staged for every pass; or a chunk at a time, in two
+    // buffers where it is copied
+    const int mine = b_hi > b_lo ? b_hi - b_lo : 0;
+    const bool once = buffer_bytes<T>(m, SLOTS, G, mine) <= share_at<T, MT>();
+    const bool copies = RAW && p.copies;
+    const int two = blocks_that_fit<T>(m, SLOTS, G, share_at<T, MT>() / 2) / step * step;
+    const bool ahead = !once && copies && two > 0;
+    const int chunk = once ? mine : (ahead ? two : blocks_that_fit<T>(m, SLOTS, G, share_at<T, MT>()) / step * step);
+    const int in_chunk = once ? (sets > 0 ? sets : 1) : chunk / step;    // sets
+    const int RB = chunk * 256, sums_in = sums_at<T>(m, chunk);          // bytes of a token's components
+    const int buf_bytes = sums_in;                                       // (of two: without sums)
     const float start = g.mins ? -16.0f : -24.0f;
+    const int k_hi = b_hi * BLOCK < K ? b_hi * BLOCK : K;
     // the row of each token, looked up once
     __shared__ int row_of[16 * MT];
     if ((int)threadIdx.x < m) {
         const int64_t r = t.first + threadIdx.x, at = g.rows ? g.rows[r] : r;
         row_of[threadIdx.x] = at >= 0 && at < g.xrows ? (int)at : -1;
     }
-    typedef vec<T, 8> run_t;
-    auto fetch = [&](int u, int runs, int c0) {
-        const int at = row_of[u / runs];
-        run_t v = run_t{};
-        if (at >= 0)
-            v = *reinterpret_cast<const run_t *>(static_cast<const T *>(g.X) + at * g.ldx + c0 + u % runs * 8);
-        return v;
-    };
-    // run u (eight indices of a token) into the buffer; the threads of a group are
-    // neighbours, and all of them are here: a chunk is whole groups
-    auto deposit = [&](char *buf, int u, int runs, const run_t &v) {
-        const int tok = u / runs, k = u % runs * 8;
-        frag<float> x;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-        float sum = ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-#pragma unroll
-        for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor(sum, d);
-        if (k % G == 0) reinterpret_cast<float *>(buf + sums_at)[k / G * TOKENS + tok] = sum * start;
-        frag<float> f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[field_place(i)] = x[i];
-#pragma unroll
-        for (int c = 0; c < PL; ++c) {
-            const frag<C> w = __builtin_convertvector(f, frag<C>);
-            *reinterpret_cast<frag<C> *>(buf + (c * m + tok) * RS + k * 2) = w;
-            if (c + 1 < PL) f = f - __builtin_convertvector(w, frag<float>);
+    // unit u (eight entries) of a token lies at (u ^ token % 16)
+    auto place = [&](int c, int tok, int unit) { return (c * m + tok) * RB + ((unit ^ (tok & 15)) << 4); };
+    // starts the copies of the chunk from block b on
+    auto copy = [&](char *buf, int b) {
+        const int units = chunk * 16, total = m * units;
+        for (int c = wave; c * 64 < total; c += WAVES) {
+            const int i = c * 64 + lane < total ? c * 64 + lane : total - 1, tok = i / units;
+            const int k = b * BLOCK + ((i - tok * units) ^ (tok & 15)) * 8;
+            const int kc = k < k_hi ? k : b * BLOCK;  // past the end: something, not used
+            const T *const src = row_of[tok] < 0 ? reinterpret_cast<const T *>(g_zero16)
+                                                 : static_cast<const T *>(g.X) + row_of[tok] * g.ldx + kc;
+            copy_lanes(reinterpret_cast<const char *>(src), buf + c * 1024);
         }
     };
-    // indices of the chunk that starts with block b
-    auto chunk_runs = [&](int b) {
-        const int hi = b_hi * BLOCK < K ? b_hi * BLOCK : K, len = hi - b * BLOCK;
-        return (len < chunk * BLOCK ? len : chunk * BLOCK) / 8;
-    };
-    auto stage = [&](int b) {
-        const int runs = chunk_runs(b);
-        for (int u = threadIdx.x; u < m * runs; u += THREADS) deposit(lds, u, runs, fetch(u, runs, b * BLOCK));
+    // the same by loads and stores, prepared on the way; the threads of a group
+    // are neighbours, and all of them are here: a chunk is whole groups
+    auto stage = [&](char *buf, int b) {
+        const int left_k = k_hi - b * BLOCK, runs = (left_k < chunk * BLOCK ? left_k : chunk * BLOCK) / 8;
+        for (int u = threadIdx.x; u < m * runs; u += THREADS) {
+            const int tok = u / runs, unit = u % runs, at = row_of[tok];
+            vec<T, 8> v = vec<T, 8>{};
+            if (at >= 0)
+                v = *reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(g.X) + at * g.ldx + b * BLOCK + unit * 8);
+            if constexpr (RAW) {
+                *reinterpret_cast<vec<T, 8> *>(buf + place(0, tok, unit)) = v;
+            } else {
+                frag<float> f = __builtin_convertvector((frag<T>)v, frag<float>);
+                float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+#pragma unroll
+                for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor(sum, d);
+                if (unit % (G / 8) == 0)
+                    reinterpret_cast<float *>(buf + sums_in)[unit / (G / 8) * TOKENS + tok] = sum * start;
+#pragma unroll
+                for (int c = 0; c < PL; ++c) {
+                    const frag<C> w = __builtin_convertvector(f, frag<C>);
+                    *reinterpret_cast<frag<C> *>(buf + place(c, tok, unit)) = to_fields(w);
+                    if (c + 1 < PL) f = f - __builtin_convertvector(w, frag<float>);
+                }
+            }
+        }
     };
 
     // a set: U neighbouring blocks of the wave's NT column tiles.  The scales of
@@ -245,30 +283,49 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     };
 
     sums_t y[NT][MT] = {};
-    int tok_at[MT];
+    int at[MT][4];                  // the lane's units of a block
 #pragma unroll
     for (int a = 0; a < MT; ++a) {
-        const int tok = FEW ? (lane & 15) / 4 : 16 * a + (lane & 15);
-        tok_at[a] = (tok < m ? tok : m - 1) * RS + h * 16;
+        const int want = FEW ? (lane & 15) / 4 : 16 * a + (lane & 15), tok = want < m ? want : m - 1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) at[a][j] = place(0, tok, 4 * j + h);
     }
+    frag<C> ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (C)1.0f;
     Set now, next;
     point(0);
     if (sets > 0) load(now, 0);
     __syncthreads();                                  // row_of
-    char *const buf = lds;
+    if (sets > 0 && copies) copy(lds, b_lo);          // (the only chunk, or the first)
+    int buf_at = ahead ? buf_bytes : 0;               // the next trip's chunk is in the other buffer
     // the sets of all passes; without any (K = 0), the passes alone
     int pass = 0, set = 0;
     do {
         if (sets > 0) {
             if (set % in_chunk == 0 && (!once || pass == 0)) {
-                if (pass + set > 0) __syncthreads();  // every wave is done with the chunk before
-                stage(b_lo + set * step);
-                __syncthreads();
+                const int b = b_lo + set * step;
+                if (ahead) {
+                    // its copies have landed, and every wave is done with the other buffer
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    __syncthreads();
+                    copy(lds + buf_at, b + chunk < b_hi ? b + chunk : b_lo);
+                    buf_at = buf_bytes - buf_at;
+                } else {
+                    if (pass + set > 0) {
+                        __syncthreads();              // every wave is done with the chunk before
+                        if (copies) copy(lds, b);
+                    }
+                    if (!copies) stage(lds, b);
+                    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                    __syncthreads();
+                }
             }
+            char *const buf = lds + buf_at;
             // the set after this one, or the next pass's first (after the last, that again)
             if (set + 1 == sets && pass + 1 < passes) point(pass + 1);
             load(next, set + 1 < sets ? set + 1 : (pass + 1 < passes ? 0 : set));
-            const float *const sums = reinterpret_cast<const float *>(buf + sums_at);
+            const float *const sums = reinterpret_cast<const float *>(buf + sums_in);
             // block u of the set; whole: all of its indices are there
             auto multiply = [&](int u, auto whole) __attribute__((always_inline)) {
                 const int b = block_of(set, u);
@@ -280,7 +337,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
                     for (int j = 0; j < 4; ++j) w[i][j] = now.w[u][i][j];
                     exchange_quarters(w[i]);
                 }
-                f32x4 acc[NT][MT];
+                f32x4 acc[NT][MT], xs[MT];            // xs: the sums of x (raw)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (!decltype(whole)::value && b * BLOCK + 32 * j >= K) break;
@@ -288,10 +345,13 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
                     if (32 * j % G == 0) {
 #pragma unroll
                         for (int a = 0; a < MT; ++a) {
-                            const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
                             f32x4 c = {};
+                            if constexpr (!RAW) {
+                                const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
 #pragma unroll
-                            for (int r = 0; r < REGS; ++r) c[r] = v[r];
+                                for (int r = 0; r < REGS; ++r) c[r] = v[r];
+                            }
+                            xs[a] = c;
 #pragma unroll
                             for (int i = 0; i < NT; ++i) acc[i][a] = c;
                         }
@@ -300,9 +360,14 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
 #pragma unroll
                     for (int a = 0; a < MT; ++a)
 #pragma unroll
-                        for (int c = 0; c < PL; ++c)
-                            x[a][c] = *reinterpret_cast<const frag<C> *>(buf + tok_at[a] + c * m * RS +
-                                                                         (in * BLOCK + 32 * j) * 2);
+                        for (int c = 0; c < PL; ++c) {
+                            x[a][c] = *reinterpret_cast<const frag<C> *>(buf + at[a][j] + c * m * RB + in * 256);
+                            if constexpr (RAW) x[a][c] = to_fields(x[a][c]);
+                        }
+                    if constexpr (RAW) {
+#pragma unroll
+                        for (int a = 0; a < MT; ++a) xs[a] = mfma16(x[a][0], ones, xs[a]);
+                    }
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
                         const frag<C> wf = sixteen_plus<C>(w[i][j]);
@@ -320,14 +385,23 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
 #pragma unroll
                             for (int a = 0; a < MT; ++a)
 #pragma unroll
-                                for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(acc[i][a][r], s, y[i][a][r]);
+                                for (int r = 0; r < REGS; ++r) {
+                                    float v = acc[i][a][r];
+                                    if constexpr (RAW) v = fmaf(xs[a][r], start, v);
+                                    y[i][a][r] = fmaf(v, s, y[i][a][r]);
+                                }
                             if (g.mins) {
-                                const float o = (float)now.o[i][u * GB + 32 * j / G] * (1.0f / -16.0f);  // of start
+                                const float o = (float)now.o[i][u * GB + 32 * j / G] * (RAW ? 1.0f : 1.0f / -16.0f);    // of start
 #pragma unroll
                                 for (int a = 0; a < MT; ++a) {
-                                    const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
+                                    if constexpr (!RAW) {
+                                        const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
 #pragma unroll
-                                    for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(v[r], o, y[i][a][r]);
+                                        for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(v[r], o, y[i][a][r]);
+                                    } else {
+#pragma unroll
+                                        for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(xs[a][r], o, y[i][a][r]);
+                                    }
                                 }
                             }
                         }
@@ -382,6 +456,8 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
         }
         ++pass;
     } while (pass < passes);
+    // the last copies may not be read: they must land before the workgroup ends
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 
 template <typename T, int MT, int NT, int U, int G>
@@ -421,16 +497,20 @@ template <typename T, int MT, int NT, int U>
 Q4Plan plan_q4(const Q4Gemm &g) {
     Q4Plan p = {};
     const int tokens = g.R < 16 * MT ? (int)g.R : 16 * MT;
-    const int blocks = (g.K + BLOCK - 1) / BLOCK, fit = blocks_that_fit<T, MT>(tokens, 16 * MT, g.group);
+    const int blocks = (g.K + BLOCK - 1) / BLOCK;
+    const bool once = buffer_bytes<T>(tokens, 16 * MT, g.group, blocks) <= share_at<T, MT>();
+    const int bufs = Q4Elem<T>::PLANES == 1 ? 2 : 1;
+    int fit = once ? blocks : blocks_that_fit<T>(tokens, 16 * MT, g.group, share_at<T, MT>() / bufs);
+    if (fit < U) fit = U;
     const int64_t rows = likely_tiles(g, 16 * MT);
     auto col_tiles = [&](int wk) { return (g.N + 16 * NT * (WAVES / wk) - 1) / (16 * NT * (WAVES / wk)); };
     // waves along the columns, as long as there are 16 waves for each CU
     p.wk = WAVES;
-    while (p.wk > 1 && (p.wk * U > fit || rows * col_tiles(p.wk / 2) * WAVES >= 16 * 256)) p.wk /= 2;
-    // few workgroups with long reductions: more along the reduction
+    while (p.wk > 1 && ((!once && p.wk * U > fit) || rows * col_tiles(p.wk / 2) * WAVES >= 16 * 256)) p.wk /= 2;
+    // few workgroups: more along the reduction, each with a set or more for its waves
     const int64_t tiles = rows * col_tiles(p.wk);
     p.splits = 1;
-    while (p.splits < 16 && tiles * p.splits * 2 <= 256 && blocks / (p.splits * 2) >= 4 * p.wk * U) p.splits *= 2;
+    while (p.splits < 16 && tiles * p.splits * 2 <= 256 && blocks / (p.splits * 2) >= 2 * p.wk * U) p.splits *= 2;
     // more workgroups than run at a time: column tiles one after the other in
     // each, so that x is staged once for them and the loads never pause
     p.passes = 1;
@@ -454,6 +534,7 @@ hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
             }
             p.part = reinterpret_cast<float *>(w);
         }
+        p.copies = reinterpret_cast<uintptr_t>(g.X) % 16 == 0 && g.ldx % 8 == 0;
         const int cols = 16 * NT * (WAVES / p.wk) * p.passes;
         const int64_t tiles = row_blocks_bound(g.R, g.E, 16 * MT) * ((g.N + cols - 1) / cols);
         q4_gemm_kernel<T, MT, NT, U, decltype(group)::value><<<dim3((unsigned)tiles, p.splits), 64 * WAVES, 0, s>>>(g, p);
