@@ -224,7 +224,7 @@ int emu_set_sgemm_split(int mode);
    Matrices are row-major with leading dimensions in elements, at any element's
    alignment; index arrays are int32.  Device pointers, ordered on the current
    stream, no host synchronisation; only emu_moe_route (more than 64 tokens)
-   and emu_q4_gemm (few rows) use the workspace.
+   and emu_q4_gemm (a reduction that is split) use the workspace.
    offsets: E + 1 entries, rows [offsets[e], offsets[e + 1]) belong to expert e
    (offsets[0] counts as 0); an expert may have none.  Rows from offsets[E] on
    belong to no expert: their outputs are zero and their inputs are not used.
@@ -235,7 +235,8 @@ int emu_set_sgemm_split(int mode);
    EMU_EINVAL (before any HIP call) for a bad type, negative sizes, a leading
    dimension below its row length, a NULL pointer to something that is not
    empty, or sizes beyond the limits given.  At most 2^24 - 1 tokens, 2^31 - 1
-   rows and 2^30 - 1 columns; E at most 2^16. */
+   rows and 2^30 - 1 columns; E at most 2^16; the leading dimensions of the
+   grouped products at most 2^31 - 1. */
 #define EMU_F32 0
 #define EMU_BF16 1
 #define EMU_F16 2
@@ -303,8 +304,8 @@ int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, co
                 int64_t ldx, int64_t XR, const int32_t *rows, const uint8_t *Q, const void *scales,
                 const void *mins, const int32_t *offsets, void *Y, int64_t ldy);
 /* Q and scales of `rows` rows of K entries (ldw): s = max |w| / 7 of the group,
-   rounded to the call's type, q = 8 + the integer nearest w / s (ties to even) within -8 .. 7 (8 where s = 0;
-   w must be finite). */
+   rounded to the call's type, q = 8 + the integer nearest w / s (ties to even)
+   within -8 .. 7 (8 where s = 0; w must be finite). */
 int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, int64_t ldw, uint8_t *Q,
                 void *scales);
 

@@ -19,9 +19,11 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libemu.so")
 SOURCES = ["split.hip", "gemm_f32.hip", "gemm_f64.hip", "gemm_f64s.hip", "gemm_f64t.hip",
            "gemm_f64w.hip", "fallback.hip", "kbin.hip", "emu_api.hip", "moe_route.hip",
-           "moe_combine.hip", "grouped.hip", "grouped16.hip", "grouped16_gemm_bf16.hip",
+           "moe_combine.hip", "grouped.hip", "grouped16_gemm_bf16.hip",
            "grouped16_gemm_f16.hip", "grouped16_wgrad_bf16.hip", "grouped16_wgrad_f16.hip",
-           "grouped32.hip", "q4.hip", "q4_f32.hip", "q4_bf16.hip", "q4_f16.hip", "moe_api.hip"]
+           "grouped_few.hip", "grouped_staged_f32.hip", "grouped_staged_bf16.hip",
+           "grouped_staged_f16.hip", "q4.hip", "q4_f32.hip", "q4_bf16.hip", "q4_f16.hip",
+           "moe_api.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,244 @@
+// The grouped product for a few rows of each expert, bound by the bytes of the
+// experts' matrices: every entry of W goes from memory to the registers of one
+// wave, from there to the matrix instructions, and is not staged.
+//
+// v_mfma 16 x 16 x 32 with rows of X as rows and 16 columns of Y as columns.  A
+// wave takes 64 columns (four tiles) and 32 indices at a time:
+//   W stored N x K: tile i is columns 16 i .. 16 i + 15, a lane loads eight
+//     neighbouring indices of a column;
+//   W stored K x N: a lane loads four neighbouring columns 4 l .. 4 l + 3 of eight
+//     indices, and tile i is the columns 4 l + i: what a lane has loaded is what
+//     the instructions want of it, with no exchange, and a row of 64 columns is
+//     one run in memory.
+// X lies in LDS (FP32 as three BF16 components, Eq. fp32split; W is split in
+// registers), the 16-byte units of row t permuted by t % 16 so that the 16 rows of a
+// read touch every bank once.  The waves of a workgroup share the reduction and
+// add up their sums in LDS at the end, in order.
+#include "moe.h"
+#include "moe_common.h"
+
+namespace emu {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+using frag = T __attribute__((ext_vector_type(8)));
+
+constexpr int WAVES = 8, THREADS = 64 * WAVES, NT = 4, COLS = 16 * NT, STEP = 32;
+constexpr int X_BYTES = 64 * 1024;          // of LDS, for X
+
+template <typename T>
+struct Elem {
+    using comp = T;
+    static constexpr int PLANES = 1;
+};
+template <>
+struct Elem<float> {
+    using comp = bhalf;
+    static constexpr int PLANES = 3;
+};
+
+__device__ __forceinline__ f32x4 mfma16(frag<bhalf> a, frag<bhalf> b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(frag<half> a, frag<half> b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+// The components of eight entries.
+template <typename T>
+__device__ __forceinline__ void components(const frag<T> &x, frag<typename Elem<T>::comp> (&c)[Elem<T>::PLANES]) {
+    if constexpr (Elem<T>::PLANES == 1) {
+        c[0] = x;
+    } else {
+        frag<float> r = x;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            c[i] = __builtin_convertvector(r, frag<bhalf>);
+            if (i < 2) r = r - __builtin_convertvector(c[i], frag<float>);
+        }
+    }
+}
+
+// What a wave has loaded of W: 32 indices of its 64 columns.
+template <typename T, bool TB>
+struct Piece;
+template <typename T>
+struct Piece<T, true> {
+    frag<T> w[NT];
+    // col: the lane's column of each tile; k: of its eight indices
+    __device__ __forceinline__ void load(const T *W, int64_t ld, int col0, int N, int k0, int K, int lane) {
+        const int k = k0 + 8 * (lane >> 4);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int n = col0 + 16 * i + (lane & 15);
+            const T *const p = W + (int64_t)(n < N ? n : N - 1) * ld + k;
+            if (k0 + STEP <= K) {
+                w[i] = *reinterpret_cast<const vec<T, 8> *>(p);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[i][j] = k + j < K ? p[j] : T(0);
+            }
+        }
+    }
+    __device__ __forceinline__ frag<T> tile(int i) const { return w[i]; }
+    static __device__ __forceinline__ int column(int i, int c) { return 16 * i + c; }
+};
+template <typename T>
+struct Piece<T, false> {
+    vec<T, NT> w[8];
+    __device__ __forceinline__ void load(const T *W, int64_t ld, int col0, int N, int k0, int K, int lane) {
+        const int k = k0 + 8 * (lane >> 4), n = col0 + 4 * (lane & 15);
+        if (k0 + STEP <= K && col0 + COLS <= N) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const vec<T, NT> *>(W + (int64_t)(k + j) * ld + n);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+                    w[j][i] = k + j < K ? W[(int64_t)(k + j) * ld + (n + i < N ? n + i : N - 1)] : T(0);
+        }
+    }
+    __device__ __forceinline__ frag<T> tile(int i) const {
+        frag<T> f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = w[j][i];
+        return f;
+    }
+    static __device__ __forceinline__ int column(int i, int c) { return 4 * c + i; }
+};
+
+template <typename T, int MT, bool TB>
+__global__ __launch_bounds__(THREADS, 2) void few_kernel(GroupedGemm g) {
+    using C = typename Elem<T>::comp;
+    constexpr int PL = Elem<T>::PLANES;
+    __shared__ __attribute__((aligned(16))) char lds[X_BYTES];
+    __shared__ float share[WAVES * MT * 256];
+    __shared__ int row_of[16 * MT];
+    const RowTile t = RowTiles(g.offsets, g.E, g.R, 16 * MT, (g.N + COLS - 1) / COLS).at(blockIdx.x);
+    if (t.e < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4;
+    const int m = (int)(t.end - t.first), K = g.K, N = g.N, col0 = t.col * COLS;
+    T *const Y = static_cast<T *>(g.Y);
+    if (t.e == g.E) {                                 // rows of no expert
+        for (int i = threadIdx.x; i < m * COLS; i += THREADS)
+            if (col0 + i % COLS < N) Y[(t.first + i / COLS) * g.ldy + col0 + i % COLS] = T(0.0f);
+        return;
+    }
+    const T *const W = static_cast<const T *>(g.W) + t.e * g.sw;
+    // steps of 32 indices: the waves take neighbouring ones; X for `chunk` of them at a time
+    const int steps = (K + STEP - 1) / STEP, rounds = (steps + WAVES - 1) / WAVES;
+    const int fit = X_BYTES / (PL * m * STEP * 2) / WAVES * WAVES;
+    const int chunk = rounds * WAVES < fit ? rounds * WAVES : fit, RB = chunk * STEP * 2;
+    const int in_chunk = chunk / WAVES;               // rounds
+    if ((int)threadIdx.x < m) {
+        const int64_t r = t.first + threadIdx.x, at = g.rows ? g.rows[r] : r;
+        row_of[threadIdx.x] = at >= 0 && at < g.xrows ? (int)at : -1;
+    }
+    f32x4 hi[NT][MT] = {}, lo[PL > 1 ? NT : 1][PL > 1 ? MT : 1] = {};
+    int at[MT];
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {
+        const int tok = 16 * a + (lane & 15) < m ? 16 * a + (lane & 15) : m - 1;
+        at[a] = tok;
+    }
+    // the 16-byte unit of row tok, plane c
+    auto place = [&](int c, int tok, int unit) { return (c * m + tok) * RB + ((unit ^ (tok & 15)) << 4); };
+    Piece<T, TB> now, next;
+    auto k_of = [&](int round) {
+        const int s = round * WAVES + wave;
+        return (s < steps ? s : steps - 1) * STEP;    // past the end: the last ones, not used
+    };
+    if (rounds > 0) now.load(W, g.ldw, col0, N, k_of(0), K, lane);
+    __syncthreads();                                  // row_of
+    for (int round = 0; round < rounds; ++round) {
+        if (round % in_chunk == 0) {
+            if (round > 0) __syncthreads();           // every wave is done with the chunk before
+            const int k0 = round * WAVES * STEP, units = chunk * STEP / 8;
+            for (int u = threadIdx.x; u < m * units; u += THREADS) {
+                const int tok = u / units, unit = u % units, k = k0 + unit * 8;
+                frag<T> x = frag<T>{};
+                if (row_of[tok] >= 0 && k < K) {
+                    const T *const p = static_cast<const T *>(g.X) + row_of[tok] * g.ldx + k;
+                    if (k + 8 <= K) {
+                        x = *reinterpret_cast<const vec<T, 8> *>(p);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = k + j < K ? p[j] : T(0);
+                    }
+                }
+                frag<C> c[PL];
+                components<T>(x, c);
+#pragma unroll
+                for (int i = 0; i < PL; ++i) *reinterpret_cast<frag<C> *>(lds + place(i, tok, unit)) = c[i];
+            }
+            __syncthreads();
+        }
+        next.load(W, g.ldw, col0, N, k_of(round + 1 < rounds ? round + 1 : round), K, lane);
+        if (round * WAVES + wave < steps) {
+            const int unit = (round % in_chunk * WAVES + wave) * (STEP / 8) + h;
+            frag<C> x[MT][PL];
+#pragma unroll
+            for (int a = 0; a < MT; ++a)
+#pragma unroll
+                for (int c = 0; c < PL; ++c) x[a][c] = *reinterpret_cast<const frag<C> *>(lds + place(c, at[a], unit));
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                frag<C> w[PL];
+                components<T>(now.tile(i), w);
+#pragma unroll
+                for (int a = 0; a < MT; ++a) {
+                    hi[i][a] = mfma16(x[a][0], w[0], hi[i][a]);
+                    if constexpr (PL > 1) {
+#pragma unroll
+                        for (int s = 2; s > 0; --s)   // A_c B_d with c + d = 2, then 1
+#pragma unroll
+                            for (int c = 0; c <= s; ++c) lo[i][a] = mfma16(x[a][c], w[s - c], lo[i][a]);
+                    }
+                }
+            }
+        }
+        now = next;
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        if (i > 0) __syncthreads();
+#pragma unroll
+        for (int a = 0; a < MT; ++a)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float v = hi[i][a][r];
+                if constexpr (PL > 1) v += lo[i][a][r];
+                share[(wave * MT + a) * 256 + (4 * h + r) * 16 + (lane & 15)] = v;
+            }
+        __syncthreads();
+        for (int j = threadIdx.x; j < m * 16; j += THREADS) {
+            const int tok = j / 16, c = j % 16, col = col0 + Piece<T, TB>::column(i, c);
+            if (col >= N) continue;
+            float v = 0.0f;
+            for (int w = 0; w < WAVES; ++w) v += share[(w * MT + tok / 16) * 256 + tok % 16 * 16 + c];
+            Y[(t.first + tok) * g.ldy + col] = (T)v;
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_few(const GroupedGemm &g, hipStream_t s) {
+    auto run = [&](auto z, auto mt, auto tb) {
+        const int64_t tiles = row_blocks_bound(g.R, g.E, 16 * decltype(mt)::value) * ((g.N + COLS - 1) / COLS);
+        few_kernel<decltype(z), decltype(mt)::value, decltype(tb)::value><<<(unsigned)tiles, THREADS, 0, s>>>(g);
+    };
+    with_type(g.dtype, [&](auto z) {
+        auto layout = [&](auto mt) {
+            if (g.transb) run(z, mt, std::true_type{});
+            else run(z, mt, std::false_type{});
+        };
+        if (g.R <= 16 * (int64_t)g.E) layout(std::integral_constant<int, 1>{});
+        else layout(std::integral_constant<int, 2>{});
+    });
+    return hipGetLastError();
+}
+
+}  // namespace emu

@@ -46,20 +46,22 @@ struct GroupedWgrad {
 };
 hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s);
 
-// The kernels of 16-bit operands copied straight to LDS: whether a call can take
-// them, and their launches with square output tiles of 128 or 256.
-bool direct_gemm(const GroupedGemm &g);
-bool direct_wgrad(const GroupedWgrad &g);
-hipError_t launch_direct_gemm(const GroupedGemm &g, int tile, hipStream_t s);
-hipError_t launch_direct_wgrad(const GroupedWgrad &g, int tile, hipStream_t s);
-// one source file each: they take long to compile
+// The kernels of 16-bit operands copied straight to LDS (grouped16.h), with square
+// output tiles of 128 or 256; one source file each: they take long to compile.
 hipError_t launch_gemm16_bf16(const GroupedGemm &g, int tile, hipStream_t s);
 hipError_t launch_gemm16_f16(const GroupedGemm &g, int tile, hipStream_t s);
 hipError_t launch_wgrad16_bf16(const GroupedWgrad &g, int tile, hipStream_t s);
 hipError_t launch_wgrad16_f16(const GroupedWgrad &g, int tile, hipStream_t s);
-// The kernels of FP32 operands on tiles of 256 x 128.
-hipError_t launch_gemm32(const GroupedGemm &g, hipStream_t s);
-hipError_t launch_wgrad32(const GroupedWgrad &g, hipStream_t s);
+// The kernels staged through registers (grouped_staged.h).
+hipError_t launch_staged_gemm_f32(const GroupedGemm &g, hipStream_t s);
+hipError_t launch_staged_gemm_bf16(const GroupedGemm &g, hipStream_t s);
+hipError_t launch_staged_gemm_f16(const GroupedGemm &g, hipStream_t s);
+hipError_t launch_staged_wgrad_f32(const GroupedWgrad &g, hipStream_t s);
+hipError_t launch_staged_wgrad_bf16(const GroupedWgrad &g, hipStream_t s);
+hipError_t launch_staged_wgrad_f16(const GroupedWgrad &g, hipStream_t s);
+// The kernel for a few rows of each expert: at most FEW_ROWS of each on average.
+constexpr int64_t FEW_ROWS = 32;
+hipError_t launch_few(const GroupedGemm &g, hipStream_t s);
 
 // Products with 4-bit matrices; see emu_q4_gemm and emu_q4_pack.
 struct Q4Gemm {

@@ -1,6 +1,8 @@
 // Entry points of the mixture-of-experts operators declared in include/emu.h:
 // argument checks (before any HIP call), degenerate sizes and launches on the
 // current stream.
+#include <initializer_list>
+
 #include "api_state.h"
 #include "moe.h"
 #include "moe_common.h"
@@ -36,6 +38,13 @@ int check_combine(int dtype, int64_t T, int64_t D, int k, int64_t R) {
     if (T < 0 || T > MAX_TOKENS || D < 0 || D > MAX_COLS || R < 0 || R > MAX_ROWS)
         return api_fail(EMU_EINVAL, "T, D or R out of range");
     if (k < 1 || k > ROUTE_CHOICES) return api_fail(EMU_EINVAL, "k must be 1 to 32");
+    return EMU_OK;
+}
+
+// Leading dimensions of the grouped products: 32-bit multiples in the kernels.
+int check_lds(std::initializer_list<int64_t> lds) {
+    for (int64_t ld : lds)
+        if (ld > MAX_ROWS) return api_fail(EMU_EINVAL, "leading dimension above 2^31 - 1");
     return EMU_OK;
 }
 
@@ -129,7 +138,11 @@ int emu_grouped_gemm(int dtype, char transb, int E, int64_t R, int64_t N, int64_
         return api_fail(EMU_EINVAL, "leading dimension below the row length");
     if (stride < 0) return api_fail(EMU_EINVAL, "stride < 0");
     if (R > 0 && N > 0 && (!Y || (K > 0 && E > 0 && (!X || !W)))) return api_fail(EMU_EINVAL, "NULL pointer");
-    if (row_blocks_bound(R, E, 32) * ((N + 127) / 128) > MAX_TILES) return api_fail(EMU_EINVAL, "product too large");
+    if (int rc = check_lds({ldx, ldw, ldy})) return rc;
+    // workgroups of 512 threads: on tiles of 16 x 64 or more where the rows are few, else of 128 x 128
+    const int64_t tiles = R <= FEW_ROWS * E ? row_blocks_bound(R, E, 16) * ((N + 63) / 64)
+                                            : row_blocks_bound(R, E, 128) * ((N + 127) / 128);
+    if (tiles > MAX_TILES / 2) return api_fail(EMU_EINVAL, "product too large");
     api_clear_error();
     if (R == 0 || N == 0) return EMU_OK;
     const GroupedGemm g = {dtype, E, (int)N, (int)K, R, XR, X, W, Y, ldx, ldw, stride, ldy, offsets, rows, tb};
@@ -146,9 +159,10 @@ int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64
         return api_fail(EMU_EINVAL, "leading dimension below the row length");
     if (stride < 0) return api_fail(EMU_EINVAL, "stride < 0");
     if (E > 0 && N > 0 && K > 0 && (!dW || (R > 0 && (!X || !dY)))) return api_fail(EMU_EINVAL, "NULL pointer");
+    if (int rc = check_lds({ldx, lddy, ldw})) return rc;
     if (E > 1 && N > 0 && K > 0 && stride < ((tb ? N : K) - 1) * ldw + (tb ? K : N))
         return api_fail(EMU_EINVAL, "the matrices of dW overlap");
-    if (E * ((N + 127) / 128) * ((K + 127) / 128) > MAX_TILES) return api_fail(EMU_EINVAL, "product too large");
+    if (E * ((N + 127) / 128) * ((K + 127) / 128) > MAX_TILES / 2) return api_fail(EMU_EINVAL, "product too large");
     api_clear_error();
     if (E == 0 || N == 0 || K == 0) return EMU_OK;
     // dW as stored: X^T dY (K x N), or its transpose dY^T X

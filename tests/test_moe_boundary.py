@@ -153,3 +153,14 @@ def test_binding_q4():
                      (dict(group=48), ValueError), (dict(W=torch.zeros((4, 96))), ValueError), (dict(), TypeError)):
         with pytest.raises(err):
             emu.q4_pack(**{**dict(W=torch.zeros((4, 64)), group=64), **bad})
+
+
+def test_leading_dimensions_of_the_grouped_products(L):
+    big = 1 << 31
+    good = (2, b"N", 3, 10, 16, 8, P, 8, 10, None, P, 16, 128, P, P, 16)
+    _refused(L.emu_grouped_gemm, good, [(7, big), (11, big), (15, big)])
+    good = (2, b"N", 3, 10, 16, 8, P, 8, 10, None, P, 16, P, P, 16, 128)
+    _refused(L.emu_grouped_wgrad, _with(good, 15, 8 * big), [(7, big), (11, big), (14, big)])
+    # more tiles than a launch has workgroups
+    good = (2, b"N", 1, 1 << 30, 1 << 20, 8, P, 8, 1 << 30, None, P, 1 << 20, 1 << 23, P, P, 1 << 20)
+    assert L.emu_grouped_gemm(*good) == EINVAL
