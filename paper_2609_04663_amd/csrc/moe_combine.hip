@@ -30,36 +30,43 @@ __device__ __forceinline__ void store_some(T *p, int64_t n, const float (&x)[N])
     }
 }
 
-// A thread takes 16 bytes of one token; the grid is (tokens, chunks of D).
-template <typename T>
+// A thread takes 16 bytes of one token, AHEAD rows of z in flight; the grid is (tokens,
+// chunks of D).
+template <typename T, int AHEAD>
 __global__ __launch_bounds__(256) void combine_kernel(const T *__restrict__ Z, int64_t ldz, int64_t R,
                                                       int64_t D, int k, const int *__restrict__ slots,
                                                       const float *__restrict__ weights,
                                                       T *__restrict__ Y, int64_t ldy) {
     constexpr int N = 16 / sizeof(T);
-    const int64_t t = blockIdx.x, d = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N;
-    if (d >= D) return;
-    float y[N] = {};
-    for (int j0 = 0; j0 < k; j0 += 4) {
-        float z[4][N], w[4];
+    const int64_t t = blockIdx.x, step = (int64_t)gridDim.y * blockDim.x * N;
+    for (int64_t d = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * N; d < D; d += step) {
+        float y[N] = {};
+        for (int j0 = 0; j0 < k; j0 += AHEAD) {
+            vec<T, N> z[AHEAD];
+            float w[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t at = j0 + j < k ? slots[t * k + j0 + j] : -1;
-            const bool there = at >= 0 && at < R;
-            w[j] = there ? (weights ? weights[t * k + j0 + j] : 1.0f) : 0.0f;
-            if (there) {
-                load_some<N>(Z + at * ldz + d, D - d, z[j]);
-            } else {
+            for (int j = 0; j < AHEAD; ++j) {
+                const int64_t at = j0 + j < k ? slots[t * k + j0 + j] : -1;
+                const bool there = at >= 0 && at < R;
+                w[j] = there ? (weights ? weights[t * k + j0 + j] : 1.0f) : 0.0f;
+                z[j] = vec<T, N>{};
+                if (there) {
+                    const T *const p = Z + at * ldz + d;
+                    if (d + N <= D) {
+                        z[j] = *reinterpret_cast<const vec<T, N> *>(p);
+                    } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i) z[j][i] = 0.0f;
+                        for (int i = 0; i < N; ++i) z[j][i] = d + i < D ? p[i] : T(0);
+                    }
+                }
             }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) y[i] = fmaf(w[j], (float)z[j][i], y[i]);
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) y[i] = fmaf(w[j], z[j][i], y[i]);
+        store_some<N>(Y + t * ldy + d, D - d, y);
     }
-    store_some<N>(Y + t * ldy + d, D - d, y);
 }
 
 // A workgroup takes a token: its dy stays in registers across the choices, four
@@ -128,9 +135,14 @@ hipError_t launch_combine(int dtype, const void *Z, int64_t ldz, int64_t R, int6
         using type = decltype(z);
         const int64_t chunks = (D + 16 / sizeof(type) - 1) / (16 / sizeof(type));
         const int threads = chunks <= 64 ? 64 : (chunks <= 128 ? 128 : 256);
-        const dim3 grid((unsigned)T, (unsigned)((chunks + threads - 1) / threads));
-        combine_kernel<type><<<grid, threads, 0, s>>>(static_cast<const type *>(Z), ldz, R, D, k, slots,
-                                                      weights, static_cast<type *>(Y), ldy);
+        const int64_t parts = (chunks + threads - 1) / threads;
+        const dim3 grid((unsigned)T, (unsigned)(parts < 65535 ? parts : 65535));
+        auto run = [&](auto ahead) {
+            combine_kernel<type, ahead><<<grid, threads, 0, s>>>(static_cast<const type *>(Z), ldz, R, D, k, slots,
+                                                                 weights, static_cast<type *>(Y), ldy);
+        };
+        if (k <= 4) run(std::integral_constant<int, 4>{});
+        else run(std::integral_constant<int, 8>{});
     });
     return hipGetLastError();
 }
