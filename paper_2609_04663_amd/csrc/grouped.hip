@@ -27,10 +27,10 @@ static bool direct_wgrad(const GroupedWgrad &g) {
 // Rows per expert up to which the kernel for few rows is the faster one.  Measured, us,
 // that kernel and the other one, 64 experts of 2048 x 2048:
 //   16 bits, copied straight to LDS   8 rows 112 and 124, 16 rows 119 and 94
-//   float32                          32 rows 323 and 615 ('T' 370 and 433),
+//   float32                          32 rows 306 and 615 ('T' 303 to 343 and 433),
 //                                    64 rows 600 and 623 ('T' 757 and 436)
-//   16 bits, 2041 x 2041 'N'         20 rows 255 and 326, 50 rows 438 and 326
-//                        'T'         10 rows 193 and 161
+//   16 bits, 2041 x 2041 'N'         30 rows 230 and 326, 50 rows 438 and 326
+//                        'T'          8 rows 191 and 161
 // A rule on the average: where the rows lie is known on the device only.
 static int64_t few_rows(const GroupedGemm &g, bool direct) {
     return g.dtype == EMU_F32 || (!direct && !g.transb) ? FEW_ROWS : 8;

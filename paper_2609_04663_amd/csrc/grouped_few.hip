@@ -13,7 +13,14 @@
 // X lies in LDS (FP32 as three BF16 components, Eq. fp32split; W is split in
 // registers), the 16-byte units of row t permuted by t % 16 so that the 16 rows of a
 // read touch every bank once.  The waves of a workgroup share the reduction and
-// add up their sums in LDS at the end, in order.
+// add up their sums in LDS at the end, in order.  FP32 needs 150 to 190 registers, so
+// a workgroup has four waves and three (two) of them share a CU; with eight only one
+// did, and its start was in the open: 43 us for 32 rows over 32 experts of 1024 x 2048
+// instead of 35.  16 bits need half of it and keep eight waves, which read longer runs
+// of a row of W ('T': 105 us instead of 125 for 64 experts of 2048 x 2048, a row each).
+//
+// That case is 537 MB (5.2 TB/s), in FP32 1074 MB in 192 us (5.6 TB/s); loads alone
+// reach 6.0 TB/s.
 #include "moe.h"
 #include "moe_common.h"
 
@@ -24,18 +31,18 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T>
 using frag = T __attribute__((ext_vector_type(8)));
 
-constexpr int WAVES = 8, THREADS = 64 * WAVES, NT = 4, COLS = 16 * NT, STEP = 32;
-constexpr int X_BYTES = 64 * 1024;          // of LDS, for X
+constexpr int NT = 4, COLS = 16 * NT, STEP = 32;
+constexpr int X_BYTES = 48 * 1024;          // of LDS, for X: room for two or three workgroups
 
 template <typename T>
 struct Elem {
     using comp = T;
-    static constexpr int PLANES = 1;
+    static constexpr int PLANES = 1, WAVES = 8;
 };
 template <>
 struct Elem<float> {
     using comp = bhalf;
-    static constexpr int PLANES = 3;
+    static constexpr int PLANES = 3, WAVES = 4;
 };
 
 __device__ __forceinline__ f32x4 mfma16(frag<bhalf> a, frag<bhalf> b, f32x4 c) {
@@ -110,9 +117,9 @@ struct Piece<T, false> {
 };
 
 template <typename T, int MT, bool TB>
-__global__ __launch_bounds__(THREADS, 2) void few_kernel(GroupedGemm g) {
+__global__ __launch_bounds__(64 * Elem<T>::WAVES, 2) void few_kernel(GroupedGemm g) {
     using C = typename Elem<T>::comp;
-    constexpr int PL = Elem<T>::PLANES;
+    constexpr int PL = Elem<T>::PLANES, WAVES = Elem<T>::WAVES, THREADS = 64 * WAVES;
     __shared__ __attribute__((aligned(16))) char lds[X_BYTES];
     __shared__ float share[WAVES * MT * 256];
     __shared__ int row_of[16 * MT];
@@ -228,7 +235,7 @@ __global__ __launch_bounds__(THREADS, 2) void few_kernel(GroupedGemm g) {
 hipError_t launch_few(const GroupedGemm &g, hipStream_t s) {
     auto run = [&](auto z, auto mt, auto tb) {
         const int64_t tiles = row_blocks_bound(g.R, g.E, 16 * decltype(mt)::value) * ((g.N + COLS - 1) / COLS);
-        few_kernel<decltype(z), decltype(mt)::value, decltype(tb)::value><<<(unsigned)tiles, THREADS, 0, s>>>(g);
+        few_kernel<decltype(z), decltype(mt)::value, decltype(tb)::value><<<(unsigned)tiles, 64 * Elem<decltype(z)>::WAVES, 0, s>>>(g);
     };
     with_type(g.dtype, [&](auto z) {
         auto layout = [&](auto mt) {
