@@ -3,7 +3,7 @@
 // wave, from there to the matrix instructions, and is not staged.
 //
 // v_mfma 16 x 16 x 32 with rows of X as rows and 16 columns of Y as columns.  A
-// wave takes 64 columns (four tiles) and 32 indices at a time:
+// wave takes 64 columns (four tiles; one, if there are few) and 32 indices at a time:
 //   W stored N x K: tile i is columns 16 i .. 16 i + 15, a lane loads eight
 //     neighbouring indices of a column;
 //   W stored K x N: a lane loads four neighbouring columns 4 l .. 4 l + 3 of eight
@@ -21,6 +21,7 @@
 //
 // That case is 537 MB (5.2 TB/s), in FP32 1074 MB in 192 us (5.6 TB/s); loads alone
 // reach 6.0 TB/s.
+#include "emu_internal.h"
 #include "moe.h"
 #include "moe_common.h"
 
@@ -31,7 +32,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T>
 using frag = T __attribute__((ext_vector_type(8)));
 
-constexpr int NT = 4, COLS = 16 * NT, STEP = 32;
+constexpr int STEP = 32;
 constexpr int X_BYTES = 48 * 1024;          // of LDS, for X: room for two or three workgroups
 
 template <typename T>
@@ -67,11 +68,11 @@ __device__ __forceinline__ void components(const frag<T> &x, frag<typename Elem<
     }
 }
 
-// What a wave has loaded of W: 32 indices of its 64 columns.
-template <typename T, bool TB>
+// What a wave has loaded of W: 32 indices of its 16 NT columns.
+template <typename T, int NT, bool TB>
 struct Piece;
-template <typename T>
-struct Piece<T, true> {
+template <typename T, int NT>
+struct Piece<T, NT, true> {
     frag<T> w[NT];
     // col: the lane's column of each tile; k: of its eight indices
     __device__ __forceinline__ void load(const T *W, int64_t ld, int col0, int N, int k0, int K, int lane) {
@@ -91,12 +92,12 @@ struct Piece<T, true> {
     __device__ __forceinline__ frag<T> tile(int i) const { return w[i]; }
     static __device__ __forceinline__ int column(int i, int c) { return 16 * i + c; }
 };
-template <typename T>
-struct Piece<T, false> {
+template <typename T, int NT>
+struct Piece<T, NT, false> {
     vec<T, NT> w[8];
     __device__ __forceinline__ void load(const T *W, int64_t ld, int col0, int N, int k0, int K, int lane) {
-        const int k = k0 + 8 * (lane >> 4), n = col0 + 4 * (lane & 15);
-        if (k0 + STEP <= K && col0 + COLS <= N) {
+        const int k = k0 + 8 * (lane >> 4), n = col0 + NT * (lane & 15);
+        if (k0 + STEP <= K && col0 + 16 * NT <= N) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = *reinterpret_cast<const vec<T, NT> *>(W + (int64_t)(k + j) * ld + n);
         } else {
@@ -113,13 +114,13 @@ struct Piece<T, false> {
         for (int j = 0; j < 8; ++j) f[j] = w[j][i];
         return f;
     }
-    static __device__ __forceinline__ int column(int i, int c) { return 4 * c + i; }
+    static __device__ __forceinline__ int column(int i, int c) { return NT * c + i; }
 };
 
-template <typename T, int MT, bool TB>
+template <typename T, int MT, int NT, bool TB>
 __global__ __launch_bounds__(64 * Elem<T>::WAVES, 2) void few_kernel(GroupedGemm g) {
     using C = typename Elem<T>::comp;
-    constexpr int PL = Elem<T>::PLANES, WAVES = Elem<T>::WAVES, THREADS = 64 * WAVES;
+    constexpr int PL = Elem<T>::PLANES, WAVES = Elem<T>::WAVES, THREADS = 64 * WAVES, COLS = 16 * NT;
     __shared__ __attribute__((aligned(16))) char lds[X_BYTES];
     __shared__ float share[WAVES * MT * 256];
     __shared__ int row_of[16 * MT];
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(64 * Elem<T>::WAVES, 2) void few_kernel(GroupedGemm
     }
     // the 16-byte unit of row tok, plane c
     auto place = [&](int c, int tok, int unit) { return (c * m + tok) * RB + ((unit ^ (tok & 15)) << 4); };
-    Piece<T, TB> now, next;
+    Piece<T, NT, TB> now, next;
     auto k_of = [&](int round) {
         const int s = round * WAVES + wave;
         return (s < steps ? s : steps - 1) * STEP;    // past the end: the last ones, not used
@@ -221,7 +222,7 @@ __global__ __launch_bounds__(64 * Elem<T>::WAVES, 2) void few_kernel(GroupedGemm
             }
         __syncthreads();
         for (int j = threadIdx.x; j < m * 16; j += THREADS) {
-            const int tok = j / 16, c = j % 16, col = col0 + Piece<T, TB>::column(i, c);
+            const int tok = j / 16, c = j % 16, col = col0 + Piece<T, NT, TB>::column(i, c);
             if (col >= N) continue;
             float v = 0.0f;
             for (int w = 0; w < WAVES; ++w) v += share[(w * MT + tok / 16) * 256 + tok % 16 * 16 + c];
@@ -233,17 +234,27 @@ __global__ __launch_bounds__(64 * Elem<T>::WAVES, 2) void few_kernel(GroupedGemm
 }  // namespace
 
 hipError_t launch_few(const GroupedGemm &g, hipStream_t s) {
-    auto run = [&](auto z, auto mt, auto tb) {
-        const int64_t tiles = row_blocks_bound(g.R, g.E, 16 * decltype(mt)::value) * ((g.N + COLS - 1) / COLS);
-        few_kernel<decltype(z), decltype(mt)::value, decltype(tb)::value><<<(unsigned)tiles, 64 * Elem<decltype(z)>::WAVES, 0, s>>>(g);
-    };
+    using std::integral_constant;
+    const int mt = g.R <= 16 * (int64_t)g.E ? 1 : 2;
+    auto tiles = [&](int nt) { return row_blocks_bound(g.R, g.E, 16 * mt) * ((g.N + 16 * nt - 1) / (16 * nt)); };
+    // 16 columns instead of 64 where the tiles would not fill the chip: 4096 x 4096, one
+    // row, 'T': 16 bits 19 -> 9.7 us, float32 42 -> 22; 'N', 16 rows, float32 58 -> 43.
+    // Not for 16 bits 'N', whose loads are then runs of 32 bytes: 8 rows 18 -> 24.
+    const int nt = tiles(4) < device_cu_count() && (g.transb || g.dtype == EMU_F32) ? 1 : 4;
     with_type(g.dtype, [&](auto z) {
-        auto layout = [&](auto mt) {
-            if (g.transb) run(z, mt, std::true_type{});
-            else run(z, mt, std::false_type{});
+        using T = decltype(z);
+        auto run = [&](auto m, auto n) {
+            constexpr int MT = decltype(m)::value, NT = decltype(n)::value, THREADS = 64 * Elem<T>::WAVES;
+            if (g.transb) few_kernel<T, MT, NT, true><<<(unsigned)tiles(NT), THREADS, 0, s>>>(g);
+            else few_kernel<T, MT, NT, false><<<(unsigned)tiles(NT), THREADS, 0, s>>>(g);
         };
-        if (g.R <= 16 * (int64_t)g.E) layout(std::integral_constant<int, 1>{});
-        else layout(std::integral_constant<int, 2>{});
+        const integral_constant<int, 1> one;
+        const integral_constant<int, 2> two;
+        const integral_constant<int, 4> four;
+        if (mt == 1 && nt == 1) run(one, one);
+        else if (mt == 1) run(one, four);
+        else if (nt == 1) run(two, one);
+        else run(two, four);
     });
     return hipGetLastError();
 }

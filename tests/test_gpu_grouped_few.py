@@ -64,3 +64,15 @@ def test_an_infinite_entry_stays_in_its_row_and_column(emu, kind):
     assert (~torch.isfinite(got[spoiled].float())).all()
     got[spoiled], Y[spoiled], S[spoiled] = 0, 0, 0
     M.check(got, Y, M.product_bar(Y, S, K, dt))
+
+
+@pytest.mark.parametrize("transb", ["N", "T"])
+@pytest.mark.parametrize("kind", list(M.TYPES))
+@pytest.mark.parametrize("R,E,N,K", [(8, 1, 17000, 70), (30, 4, 4111, 100), (60, 2, 8200, 65), (400, 60, 1000, 64)])
+def test_enough_columns_to_fill_the_chip(emu, kind, R, E, N, K, transb):
+    dt = M.TYPES[kind]
+    X, W, offsets, rows, _ = _case(R + N, R, E, N, K, dt, True)
+    Y, S = M.grouped(X, W, offsets, rows)
+    w = W if transb == "N" else W.transpose(1, 2).contiguous()
+    got = emu.grouped_gemm(X.cuda(), w.cuda(), offsets.int().cuda(), transb=transb, rows=_cuda(rows))
+    M.check(got, Y, M.product_bar(Y, S, K, dt))
