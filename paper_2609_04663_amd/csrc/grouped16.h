@@ -1,20 +1,28 @@
 // The grouped products of bfloat16 and half operands whose rows can be copied
 // straight to LDS (16-byte alignment; see direct_gemm and direct_wgrad for the
-// rule).  Same results as the kernels of grouped.hip, which serve the others.
+// rule).
 //
-// A workgroup of 2 x 2 waves computes a tile of 64 RB x 64 RB (256 x 256 or
+// A workgroup of 2 x 2 waves computes tiles of 64 RB x 64 RB (256 x 256 or
 // 128 x 128), a wave RB x RB blocks of 32 x 32, by v_mfma 32 x 32 x 16.  A
-// k-block of 32 indices of both operands is copied by global_load_lds into one
-// of four LDS stages while the MFMAs of the others run; each lane names its own
+// k-block of 64 indices of both operands is copied by global_load_lds into one
+// of two LDS stages while the MFMAs of the other run; each lane names its own
 // source, so the gather of token rows costs nothing and the 16-byte chunks are
 // permuted on the way:
-//   contiguous along the reduction (X; W stored N x K): 64 bytes a row, chunk q
-//     of row r at q ^ (r / 4 % 4); read by ds_read_b128;
+//   contiguous along the reduction (X; W stored N x K): 128 bytes a row, chunk q
+//     of row r at q ^ (r / 2 % 8); read by ds_read_b128;
 //   contiguous along the other direction (W stored K x N; both operands of the
 //     matrix gradient): 128 RB bytes an index, chunk c of index k at c ^ 4 (k % 4);
 //     read by ds_read_b64_tr_b16, which hands a lane four indices of one column.
 // Either way the 16 lanes of a read phase (32 of the 8-byte read) touch every
-// bank once.
+// bank once.  k-blocks of 32 in four stages read 64-byte rows: 5 to 9 % slower.
+//
+// A wave's 256 accumulators leave one workgroup of 256 x 256 to a CU; its tiles run
+// as one stream of k-blocks, the next tile's copies under the stores of the last.
+// Measured in bfloat16: 131072 rows over 64 experts of 1024 x 2048, gathered, 557 to
+// 610 us (0.9 to 1.0 PFLOP/s; a large library product reaches 1.47), of which the
+// partly filled last tiles of the experts are 13 % and the stores, which the next
+// tile's first copies wait for, about 100 us.  Its matrix gradient over 65536 rows:
+// 373 to 400 us (0.7 PFLOP/s), bound by the issue of copies and transposing reads.
 #pragma once
 
 #include "gemm_common.h"
@@ -42,7 +50,7 @@ __device__ __forceinline__ f32x16 mfma32(frag<half> a, frag<half> b, f32x16 c) {
 __device__ __attribute__((aligned(16))) float g_zero4[4];
 
 // The copies and fragment reads of one operand of the tile: ROWS = 64 RB tile
-// rows (or columns) by the 32 indices of a k-block.
+// rows (or columns) by the indices of a k-block.
 enum Mode { CONTIG, STRIDED };
 
 template <int RB, int MODE>
@@ -52,7 +60,7 @@ template <int RB>
 struct Side<RB, CONTIG> {
     static constexpr int ROWS = 64 * RB, BYTES = ROWS * BK * 2, COPIES = RB * BK / 32;        // per wave
     static constexpr int RS = BK * 2, Q = RS / 16;                              // a row's bytes, chunks
-    static __device__ __forceinline__ int place(int r) { return BK == 64 ? r >> 1 & 7 : r >> 2 & 3; }
+    static __device__ __forceinline__ int place(int r) { return r >> 1 & 7; }
     const char *base;               // uniform
     unsigned off[COPIES];
     int at[SUBS];                   // fragment offset per sub-step
@@ -84,7 +92,7 @@ struct Side<RB, CONTIG> {
     }
 };
 
-// Transposing reads, and the chunk that a lane copies, of a [32][ROWS] stage.
+// Transposing reads, and the chunk that a lane copies, of a [BK][ROWS] stage.
 template <int RB>
 struct StridedSide {
     static constexpr int ROWS = 64 * RB, RS = ROWS * 2, BYTES = BK * RS, COPIES = RB * BK / 32;
