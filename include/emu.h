@@ -223,8 +223,11 @@ int emu_set_sgemm_split(int mode);
    outputs NaN).  They raise no EMU_STATUS_* bits.
    Matrices are row-major with leading dimensions in elements, at any element's
    alignment; index arrays are int32.  Device pointers, ordered on the current
-   stream, no host synchronisation; only emu_moe_route (more than 64 tokens)
-   and emu_q4_gemm (a reduction that is split) use the workspace.
+   stream, no host synchronisation.  The workspace is used by emu_moe_route
+   (more than 64 tokens), emu_q4_gemm (a reduction that is split) and the
+   grouped products (16-bit operands that are copied to 16-byte alignment first,
+   sums of few matrices in pieces); the last three do without it where it cannot
+   grow.
    offsets: E + 1 entries, rows [offsets[e], offsets[e + 1]) belong to expert e
    (offsets[0] counts as 0); an expert may have none.  Rows from offsets[E] on
    belong to no expert: their outputs are zero and their inputs are not used.

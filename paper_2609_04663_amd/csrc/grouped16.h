@@ -131,11 +131,12 @@ struct Side<RB, STRIDED> : StridedSide<RB> {
     int64_t step;                   // bytes from one k-block to the next
     unsigned off[S::COPIES];
     __device__ __forceinline__ void init_lane(int, int lane, int part) { S::init_reads(lane, part); }
-    // cols: the columns that exist (a multiple of 8); copies past them repeat the last ones
+    // cols: the columns that exist (rows have them up to a multiple of 8); copies past
+    // them repeat the last ones
     __device__ __forceinline__ void init(const char *base_, int64_t ld, int64_t cols, int wave, int lane) {
         base = base_;
         step = ld * 2 * BK;
-        const int last = (int)(cols / 8) - 1;
+        const int last = (int)((cols + 7) / 8) - 1;
 #pragma unroll
         for (int c = 0; c < S::COPIES; ++c) {
             const int q = S::chunk(c, wave, lane);
@@ -173,7 +174,7 @@ struct RowSide : StridedSide<RB> {
         map = (const __attribute__((address_space(4))) int *)map_;
         entries = entries_;
         end = rows;
-        const int last = (int)(cols / 8) - 1;
+        const int last = (int)((cols + 7) / 8) - 1;
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const int q = S::chunk(c, wave, lane);
@@ -346,6 +347,27 @@ __device__ __forceinline__ void store(const f32x16 (&acc)[RB][RB], int wave, int
     }
 }
 
+// acc to FP32 C, whose rows have their columns up to a multiple of four.
+template <int RB>
+__device__ __forceinline__ void store_sums(const f32x16 (&acc)[RB][RB], int wave, int lane, int rows, int cols,
+                                           float *__restrict__ C, int64_t ldc) {
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+        const int row = ((wave >> 1) * RB + i) * 32 + (lane & 31);
+        if (row >= rows) continue;
+#pragma unroll
+        for (int j = 0; j < RB; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int col = ((wave & 1) * RB + j) * 32 + 2 * r + 4 * (lane >> 5);
+                const f32x16 &v = acc[i][j];
+                const f32x4 w = {v[r], v[r + 1], v[r + 2], v[r + 3]};
+                if (col < cols) *reinterpret_cast<f32x4 *>(C + row * ldc + col) = w;
+            }
+    }
+}
+
 constexpr int LIST = 64;            // most tiles of a workgroup
 
 // The row tiles w, w + workgroups, ... of a grouped product, found before the
@@ -480,6 +502,7 @@ __global__ __launch_bounds__(256, RB == 4 ? 1 : 2) void gemm16_kernel(GroupedGem
 template <typename T, int RB, int MAPPED>        // the operand that goes through a map: 0 none, 1 P, 2 Q
 struct WgradSource {
     static constexpr int TILE = 64 * RB;
+    static constexpr bool PIECES = RB == 2;     // an expert's rows may be in pieces (the others have no registers to spare)
     using A = RowSide<RB, MAPPED == 1>;
     using B = RowSide<RB, MAPPED == 2>;
     const GroupedWgrad &g;
@@ -487,14 +510,14 @@ struct WgradSource {
     const int64_t total;
     int64_t w;
     struct Tile {
-        int e, m, n, lo, rows;      // e: -1 for no tile
+        int e, m, n, lo, rows;      // e: piece of an expert, -1 for no tile
     } now, next;
     A a;
     B b;
     int kb, KB;                     // of the tile that a and b stand for
 
     __device__ __forceinline__ WgradSource(const GroupedWgrad &g_, int wave, int lane)
-        : g(g_), mt((g_.M + TILE - 1) / TILE), nt((g_.N + TILE - 1) / TILE), total((int64_t)g_.E * mt * nt),
+        : g(g_), mt((g_.M + TILE - 1) / TILE), nt((g_.N + TILE - 1) / TILE), total((int64_t)g_.E * (PIECES ? g_.pieces : 1) * mt * nt),
           w(blockIdx.x) {
         a.init_lane(wave, lane, wave >> 1);
         b.init_lane(wave, lane, wave & 1);
@@ -506,7 +529,8 @@ struct WgradSource {
         if (w / 8 >= per || id >= total) return {-1, 0, 0, 0, 0};
         const int e = (int)(id / (mt * nt)), r = (int)(id % (mt * nt));
         int64_t lo, hi;
-        expert_rows(g.offsets, g.E, g.R, e, lo, hi);
+        expert_rows(g.offsets, g.E, g.R, PIECES ? e / g.pieces : e, lo, hi);
+        if constexpr (PIECES) piece_rows(e % g.pieces, g.pieces, lo, hi);
         return {uniform(e), uniform(r % mt * TILE), uniform(r / mt * TILE), uniform(lo), uniform(hi - lo)};
     }
     // at least two, the missing ones zeros
@@ -553,8 +577,9 @@ struct WgradSource {
     __device__ __forceinline__ bool close(const f32x16 (&acc)[RB][RB]) {
         const int m = g.M - now.m < TILE ? g.M - now.m : TILE, n = g.N - now.n < TILE ? g.N - now.n : TILE;
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        store<T, RB>(acc, wave, lane, m, n, static_cast<T *>(g.dW) + now.e * g.sw + now.m * g.ldw + now.n, g.ldw,
-                     [](int) { return true; });
+        const int64_t at = now.e * g.sw + now.m * g.ldw + now.n;
+        if (PIECES && g.pieces > 1) store_sums<RB>(acc, wave, lane, m, n, static_cast<float *>(g.dW) + at, g.ldw);
+        else store<T, RB>(acc, wave, lane, m, n, static_cast<T *>(g.dW) + at, g.ldw, [](int) { return true; });
         now = next;
         return now.e >= 0;
     }
@@ -600,11 +625,13 @@ template <typename T>
 hipError_t launch_wgrad16(const GroupedWgrad &g, int tile, hipStream_t s) {
     auto run = [&](auto rb) {
         constexpr int RB = decltype(rb)::value, TILE = 64 * RB;
-        const int64_t tiles = (int64_t)g.E * ((g.M + TILE - 1) / TILE) * ((g.N + TILE - 1) / TILE);
+        const int64_t tiles = (int64_t)g.E * g.pieces * ((g.M + TILE - 1) / TILE) * ((g.N + TILE - 1) / TILE);
         const unsigned grid = workgroups(tiles, RB == 4 ? 1 : 2);
-        if (g.prow) wgrad16_kernel<T, RB, 1><<<grid, 256, 0, s>>>(g);
-        else if (g.qrow) wgrad16_kernel<T, RB, 2><<<grid, 256, 0, s>>>(g);
-        else wgrad16_kernel<T, RB, 0><<<grid, 256, 0, s>>>(g);
+        if constexpr (RB == 4) {
+            if (g.prow) return wgrad16_kernel<T, RB, 1><<<grid, 256, 0, s>>>(g);
+            if (g.qrow) return wgrad16_kernel<T, RB, 2><<<grid, 256, 0, s>>>(g);
+        }
+        wgrad16_kernel<T, RB, 0><<<grid, 256, 0, s>>>(g);
     };
     if (tile == 256) run(std::integral_constant<int, 4>{});
     else run(std::integral_constant<int, 2>{});

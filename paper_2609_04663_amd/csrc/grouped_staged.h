@@ -347,15 +347,16 @@ __global__ __launch_bounds__(THREADS, 2) void staged_wgrad_kernel(GroupedWgrad g
     constexpr int AROWS = 32 * WM * RB;
     __shared__ __attribute__((aligned(1024))) char lds[lds_bytes<T, AROWS>()];
     const int mt = (g.M + AROWS - 1) / AROWS, nt = (g.N + BN - 1) / BN;
-    // an XCD takes a contiguous run of tiles, so of experts
-    const int64_t total = (int64_t)g.E * mt * nt, per = (total + 7) / 8;
+    // an XCD takes a contiguous run of tiles, so of (pieces of) experts
+    const int64_t total = (int64_t)g.E * g.pieces * mt * nt, per = (total + 7) / 8;
     const int64_t id = blockIdx.x % 8 * per + blockIdx.x / 8;
     if (blockIdx.x / 8 >= per || id >= total) return;
     const int e = uniform(id / (mt * nt)), r = uniform(id % (mt * nt));
     const int m0 = r % mt * AROWS, n0 = r / mt * BN;
     const int rows = g.M - m0 < AROWS ? g.M - m0 : AROWS, cols = g.N - n0 < BN ? g.N - n0 : BN;
     int64_t lo, hi;
-    expert_rows(g.offsets, g.E, g.R, e, lo, hi);
+    expert_rows(g.offsets, g.E, g.R, e / g.pieces, lo, hi);
+    piece_rows(e % g.pieces, g.pieces, lo, hi);
     lo = uniform(lo);
     const int K = uniform(hi - lo);
     StridedLoads<T, AROWS, MAPPED == 1> a;
@@ -411,9 +412,9 @@ hipError_t run_staged_gemm(const GroupedGemm &g, hipStream_t s) {
 template <typename T>
 hipError_t run_staged_wgrad(const GroupedWgrad &g, hipStream_t s) {
     const int64_t nt = (g.N + BN - 1) / BN;
-    with_height(nt * g.E, [&](int h) { return (g.M + h - 1) / h; }, [&](auto wm, auto wn, auto rb, auto cb) {
+    with_height(nt * g.E * g.pieces, [&](int h) { return (g.M + h - 1) / h; }, [&](auto wm, auto wn, auto rb, auto cb) {
         constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value, RB = decltype(rb)::value, CB = decltype(cb)::value;
-        const int64_t tiles = g.E * nt * ((g.M + 32 * WM * RB - 1) / (32 * WM * RB));
+        const int64_t tiles = g.E * g.pieces * nt * ((g.M + 32 * WM * RB - 1) / (32 * WM * RB));
         const unsigned grid = (unsigned)((tiles + 7) / 8 * 8);
         if (g.prow) staged_wgrad_kernel<T, WM, WN, RB, CB, 1><<<grid, THREADS, 0, s>>>(g);
         else if (g.qrow) staged_wgrad_kernel<T, WM, WN, RB, CB, 2><<<grid, THREADS, 0, s>>>(g);

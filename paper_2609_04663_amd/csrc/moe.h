@@ -43,6 +43,9 @@ struct GroupedWgrad {
     void *dW;
     int64_t ldp, ldq, ldw, sw;
     const int *offsets, *prow, *qrow;   // row numbers of P and Q, or null: r itself
+    // An expert's rows in this many pieces, each with its own sum: FP32 matrices
+    // dW[e pieces + i], ldw a multiple of 4, sw entries apart.
+    int pieces;
 };
 hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s);
 

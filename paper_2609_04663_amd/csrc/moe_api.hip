@@ -167,9 +167,9 @@ int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64
     if (E == 0 || N == 0 || K == 0) return EMU_OK;
     // dW as stored: X^T dY (K x N), or its transpose dY^T X
     const GroupedWgrad g = tb ? GroupedWgrad{dtype, E, (int)N, (int)K, R, R, XR, dY, X, dW, lddy, ldx,
-                                             ldw, stride, offsets, nullptr, rows}
+                                             ldw, stride, offsets, nullptr, rows, 1}
                               : GroupedWgrad{dtype, E, (int)K, (int)N, R, XR, R, X, dY, dW, ldx, lddy,
-                                             ldw, stride, offsets, rows, nullptr};
+                                             ldw, stride, offsets, rows, nullptr, 1};
     return done(launch_grouped_wgrad(g, api_stream()), "grouped_wgrad");
 }
 

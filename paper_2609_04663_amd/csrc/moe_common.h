@@ -58,6 +58,13 @@ __device__ inline void expert_rows(const int *__restrict__ offsets, int E, int64
     hi = b < lo ? lo : (b < R ? b : R);
 }
 
+// Piece i of `pieces` of an expert's rows: multiples of 64 rows, the last the rest.
+__device__ inline void piece_rows(int i, int pieces, int64_t &lo, int64_t &hi) {
+    const int64_t per = ((hi - lo + pieces - 1) / pieces + 63) & ~(int64_t)63, first = lo + i * per;
+    lo = first < hi ? first : hi;
+    hi = lo + per < hi ? lo + per : hi;
+}
+
 // Blocks of at most `rows` rows of one expert: at most this many.
 inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
     return R / rows + (E + 1 < R ? E + 1 : R);
