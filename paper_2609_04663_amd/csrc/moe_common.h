@@ -85,6 +85,13 @@ __device__ __forceinline__ int sum_up_to_lane(int v) {
     return v;
 }
 
+// v of another lane: within 16 lanes by moves between registers (0xB1, 0x4E: the lane's
+// neighbour and the other pair of its four; 0x141, 0x140: its eight and its 16 mirrored).
+template <int CTRL, typename T>
+__device__ __forceinline__ T moved(T v) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+
 // A workgroup's block of rows and its column tile.
 struct RowTile {
     int e;                 // expert; -1: there is no such tile; E: rows of no expert

@@ -45,12 +45,6 @@ __device__ __forceinline__ float exp_below(float x, float m) {
     return x == m ? 1.0f : (x > -INFINITY ? expf(x - m) : 0.0f);
 }
 
-// v of another lane: within 16 lanes by moves between registers (0xB1, 0x4E: the lane's
-// neighbour and the other pair of its four; 0x141, 0x140: its eight and its 16 mirrored).
-template <int CTRL, typename T>
-__device__ __forceinline__ T moved(T v) {
-    return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
-}
 // f over LANES lanes (16 or 64), in all of them; f is associative and commutative but
 // for roundings, which are alike in every lane: f(a, b) and f(b, a) are.
 template <int LANES, typename T, typename F>

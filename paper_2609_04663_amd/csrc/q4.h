@@ -14,7 +14,11 @@
 // of 32 can be scaled.  x lies in LDS, the 16-byte units of token t permuted by
 // t % 16, so that the 16 tokens of a read touch every bank once.  Two forms:
 //   prepared (FP32, and tiles of at most four rows): the components in the order
-//     of the weights' fields, with the sums of each group, made as x is staged;
+//     of the weights' fields, with the sums of each group, made as x is staged; of
+//     more than 16 FP32 rows a chunk ahead, loaded to registers under the products
+//     of the chunk before.  What that costs is the same for every workgroup, so all
+//     eight waves lie along the columns there: 40 rows of 8192 x 8192 42 us, with
+//     two waves along the reduction and no fetching ahead 50;
 //   raw (more rows of 16 bits): copied as it is by global_load_lds, a chunk ahead
 //     in a second buffer where it does not fit at once; a fragment is put into the
 //     fields' order after it is read, and one more matrix instruction with ones
@@ -145,6 +149,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     constexpr int PL = Q4Elem<T>::PLANES, GB = BLOCK / G;                // groups of a block
     constexpr int REGS = FEW ? 1 : 4, TOKENS = FEW ? 4 : 16 * MT;
     constexpr bool RAW = PL == 1 && !FEW;
+    constexpr bool FETCH = PL == 3 && MT > 1;         // prepared a chunk ahead, through registers
     constexpr int SLOTS = RAW ? 0 : TOKENS;                              // sums of a group
     constexpr int THREADS = 64 * WAVES;
     static_assert(blocks_that_fit<T>(16 * MT, 16 * MT, 32, share_at<T, MT>()) >= U, "a set's blocks");
@@ -174,16 +179,16 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     const int step = wk * U, sets = b_hi > b_lo ? (b_hi - b_lo + step - 1) / step : 0;
 
     // x: all of it at once, staged for every pass; or a chunk at a time, in two
-    // buffers where it is copied
+    // buffers where it is copied or fetched ahead
     const int mine = b_hi > b_lo ? b_hi - b_lo : 0;
     const bool once = buffer_bytes<T>(m, SLOTS, G, mine) <= share_at<T, MT>();
     const bool copies = RAW && p.copies;
     const int two = blocks_that_fit<T>(m, SLOTS, G, share_at<T, MT>() / 2) / step * step;
-    const bool ahead = !once && copies && two > 0;
+    const bool ahead = !once && (copies || FETCH) && two > 0;
     const int chunk = once ? mine : (ahead ? two : blocks_that_fit<T>(m, SLOTS, G, share_at<T, MT>()) / step * step);
     const int in_chunk = once ? (sets > 0 ? sets : 1) : chunk / step;    // sets
     const int RB = chunk * 256, sums_in = sums_at<T>(m, chunk);          // bytes of a token's components
-    const int buf_bytes = sums_in;                                       // (of two: without sums)
+    const int buf_bytes = sums_in + chunk * GB * SLOTS * 4;
     const float start = g.mins ? -16.0f : -24.0f;
     const int k_hi = b_hi * BLOCK < K ? b_hi * BLOCK : K;
     // the row of each token, looked up once
@@ -208,6 +213,38 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     };
     // the same by loads and stores, prepared on the way; the threads of a group
     // are neighbours, and all of them are here: a chunk is whole groups
+    // Puts entries v of a token, unit u of the chunk, into the buffer.
+    auto prepare = [&](char *buf, int tok, int unit, const vec<T, 8> &v) {
+        if constexpr (RAW) {
+            *reinterpret_cast<vec<T, 8> *>(buf + place(0, tok, unit)) = v;
+        } else {
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = (float)v[i];
+            float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+            sum += moved<0xB1>(sum);                  // over the group's lanes
+            sum += moved<0x4E>(sum);
+            if constexpr (G >= 64) sum += moved<0x141>(sum);
+            if constexpr (G >= 128) sum += moved<0x140>(sum);
+            if (unit % (G / 8) == 0)
+                reinterpret_cast<float *>(buf + sums_in)[unit / (G / 8) * TOKENS + tok] = sum * start;
+#pragma unroll
+            for (int c = 0; c < PL; ++c) {
+                u32x4 w;                              // in the fields' order
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    typedef C c2 __attribute__((ext_vector_type(2)));
+                    const c2 pair = {(C)f[i], (C)f[i + 4]};
+                    w[i] = __builtin_bit_cast(unsigned, pair);
+                    if (c + 1 < PL) {                 // (three components: of bfloat16)
+                        f[i] -= __uint_as_float(w[i] << 16);
+                        f[i + 4] -= __uint_as_float(w[i] & 0xFFFF0000u);
+                    }
+                }
+                *reinterpret_cast<u32x4 *>(buf + place(c, tok, unit)) = w;
+            }
+        }
+    };
     auto stage = [&](char *buf, int b) {
         const int left_k = k_hi - b * BLOCK, runs = (left_k < chunk * BLOCK ? left_k : chunk * BLOCK) / 8;
         for (int u = threadIdx.x; u < m * runs; u += THREADS) {
@@ -215,22 +252,27 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
             vec<T, 8> v = vec<T, 8>{};
             if (at >= 0)
                 v = *reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(g.X) + at * g.ldx + b * BLOCK + unit * 8);
-            if constexpr (RAW) {
-                *reinterpret_cast<vec<T, 8> *>(buf + place(0, tok, unit)) = v;
-            } else {
-                frag<float> f = __builtin_convertvector((frag<T>)v, frag<float>);
-                float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+            prepare(buf, tok, unit, v);
+        }
+    };
+    // a chunk of half the LDS in registers: loaded while the chunk before is
+    // multiplied, prepared into the other buffer after it
+    constexpr int HELD = FETCH ? (share_at<T, MT>() / 2 / (PL * 256) * 16 + THREADS - 1) / THREADS : 1;
+    vec<T, 8> held[HELD];
+    auto fetch = [&](int b) {
 #pragma unroll
-                for (int d = 1; d < G / 8; d <<= 1) sum += __shfl_xor(sum, d);
-                if (unit % (G / 8) == 0)
-                    reinterpret_cast<float *>(buf + sums_in)[unit / (G / 8) * TOKENS + tok] = sum * start;
+        for (int i = 0; i < HELD; ++i) {
+            const int u = threadIdx.x + i * THREADS, tok = u / (chunk * 16), k = b * BLOCK + u % (chunk * 16) * 8;
+            held[i] = vec<T, 8>{};
+            if (tok < m && k < k_hi && row_of[tok] >= 0)
+                held[i] = *reinterpret_cast<const vec<T, 8> *>(static_cast<const T *>(g.X) + row_of[tok] * g.ldx + k);
+        }
+    };
+    auto deposit = [&](char *buf) {
 #pragma unroll
-                for (int c = 0; c < PL; ++c) {
-                    const frag<C> w = __builtin_convertvector(f, frag<C>);
-                    *reinterpret_cast<frag<C> *>(buf + place(c, tok, unit)) = to_fields(w);
-                    if (c + 1 < PL) f = f - __builtin_convertvector(w, frag<float>);
-                }
-            }
+        for (int i = 0; i < HELD; ++i) {
+            const int u = threadIdx.x + i * THREADS, tok = u / (chunk * 16), unit = u % (chunk * 16);
+            if (tok < m) prepare(buf, tok, unit, held[i]);
         }
     };
 
@@ -305,7 +347,14 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
         if (sets > 0) {
             if (set % in_chunk == 0 && (!once || pass == 0)) {
                 const int b = b_lo + set * step;
-                if (ahead) {
+                if (FETCH && ahead) {
+                    // every wave is done with the chunk before the last, whose buffer this one takes
+                    if (pass + set == 0) fetch(b);
+                    buf_at = buf_bytes - buf_at;
+                    deposit(lds + buf_at);
+                    fetch(b + chunk < b_hi ? b + chunk : b_lo);
+                    __syncthreads();
+                } else if (ahead) {
                     // its copies have landed, and every wave is done with the other buffer
                     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                     __syncthreads();
@@ -499,13 +548,13 @@ Q4Plan plan_q4(const Q4Gemm &g) {
     const int tokens = g.R < 16 * MT ? (int)g.R : 16 * MT;
     const int blocks = (g.K + BLOCK - 1) / BLOCK;
     const bool once = buffer_bytes<T>(tokens, 16 * MT, g.group, blocks) <= share_at<T, MT>();
-    const int bufs = Q4Elem<T>::PLANES == 1 ? 2 : 1;
+    const int bufs = Q4Elem<T>::PLANES == 1 || MT > 1 ? 2 : 1;
     int fit = once ? blocks : blocks_that_fit<T>(tokens, 16 * MT, g.group, share_at<T, MT>() / bufs);
     if (fit < U) fit = U;
     const int64_t rows = likely_tiles(g, 16 * MT);
     auto col_tiles = [&](int wk) { return (g.N + 16 * NT * (WAVES / wk) - 1) / (16 * NT * (WAVES / wk)); };
     // waves along the columns, as long as there are 16 waves for each CU
-    p.wk = WAVES;
+    p.wk = Q4Elem<T>::PLANES == 3 && MT > 1 ? 1 : WAVES;
     while (p.wk > 1 && ((!once && p.wk * U > fit) || rows * col_tiles(p.wk / 2) * WAVES >= 16 * 256)) p.wk /= 2;
     // few workgroups: more along the reduction, each with a set or more for its waves
     const int64_t tiles = rows * col_tiles(p.wk);
@@ -551,12 +600,14 @@ hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
         const integral_constant<int, 2> two;
         const integral_constant<int, 3> three;
         const integral_constant<int, 4> four;
-        // a wave has 4 KB of weights in flight
+        // A wave has 4 KB of weights in flight, 2 KB where FP32 leaves no registers for
+        // more.  Above 48 FP32 rows tiles of 32, whose weights are read twice: 64 rows of
+        // 4096 x 8192 take 40 us, a tile of 64, which spills, 95.
         constexpr bool wide = Q4Elem<T>::PLANES == 3;
         if (g.R <= 16 * (int64_t)g.E) run(one, one, four, group);
-        else if (g.R <= 32 * (int64_t)g.E) run(two, four, one, group);
-        else if (g.R <= 48 * (int64_t)g.E) run(three, integral_constant<int, wide ? 2 : 4>{}, integral_constant<int, wide ? 2 : 1>{}, group);
-        else run(four, two, two, group);
+        else if (g.R <= 32 * (int64_t)g.E) run(two, integral_constant<int, wide ? 2 : 4>{}, one, group);
+        else if (g.R <= 48 * (int64_t)g.E) run(three, integral_constant<int, wide ? 2 : 4>{}, one, group);
+        else run(integral_constant<int, wide ? 2 : 4>{}, two, integral_constant<int, wide ? 1 : 2>{}, group);
     };
     if (g.group == 32) rows(std::integral_constant<int, 32>{});
     else if (g.group == 64) rows(std::integral_constant<int, 64>{});
