@@ -507,8 +507,7 @@ struct WgradSource {
     using B = RowSide<RB, MAPPED == 2>;
     const GroupedWgrad &g;
     const int mt, nt;
-    const int64_t total;
-    int64_t w;
+    int id, end;                    // the next tile, and the end of the XCD's
     struct Tile {
         int e, m, n, lo, rows;      // e: piece of an expert, -1 for no tile
     } now, next;
@@ -517,17 +516,24 @@ struct WgradSource {
     int kb, KB;                     // of the tile that a and b stand for
 
     __device__ __forceinline__ WgradSource(const GroupedWgrad &g_, int wave, int lane)
-        : g(g_), mt((g_.M + TILE - 1) / TILE), nt((g_.N + TILE - 1) / TILE), total((int64_t)g_.E * (PIECES ? g_.pieces : 1) * mt * nt),
-          w(blockIdx.x) {
+        : g(g_), mt((g_.M + TILE - 1) / TILE), nt((g_.N + TILE - 1) / TILE) {
+        // an XCD has a contiguous run of tiles, so of experts, and its workgroups take them in
+        // turn.  The runs take the same time (unevenly loaded experts: 401 -> 388 us); where
+        // a workgroup has one tile at most, they are of equal length.
+        const int64_t each = (int64_t)(PIECES ? g.pieces : 1) * mt * nt, total = g.E * each, per = (total + 7) / 8;
+        const int x = blockIdx.x % 8;
+        const bool even = total <= gridDim.x;
+        const int64_t first = even ? x * per : first_tile_of_xcd(g.offsets, g.E, g.R, each, x);
+        end = uniform(even ? (first + per < total ? first + per : total)
+                           : first_tile_of_xcd(g.offsets, g.E, g.R, each, x + 1));
+        id = uniform(first) + blockIdx.x / 8;
         a.init_lane(wave, lane, wave >> 1);
         b.init_lane(wave, lane, wave & 1);
         now = next = tile();
     }
-    // the tile of workgroup w: an XCD takes a contiguous run of tiles, so of experts
     __device__ __forceinline__ Tile tile() const {
-        const int64_t per = (total + 7) / 8, id = w % 8 * per + w / 8;
-        if (w / 8 >= per || id >= total) return {-1, 0, 0, 0, 0};
-        const int e = (int)(id / (mt * nt)), r = (int)(id % (mt * nt));
+        if (id >= end) return {-1, 0, 0, 0, 0};
+        const int e = id / (mt * nt), r = id % (mt * nt);
         int64_t lo, hi;
         expert_rows(g.offsets, g.E, g.R, PIECES ? e / g.pieces : e, lo, hi);
         if constexpr (PIECES) piece_rows(e % g.pieces, g.pieces, lo, hi);
@@ -556,7 +562,7 @@ struct WgradSource {
         return true;
     }
     __device__ __forceinline__ void open() {
-        w += gridDim.x;
+        id += gridDim.x / 8;
         next = tile();
     }
     __device__ __forceinline__ void trip() {

@@ -65,6 +65,47 @@ __device__ inline void piece_rows(int i, int pieces, int64_t &lo, int64_t &hi) {
     hi = lo + per < hi ? lo + per : hi;
 }
 
+// The first of the tiles of XCD x (0 .. 8), where every expert has `each` tiles, one
+// after the other, that take a time of its rows and START more: the XCDs get
+// contiguous runs of tiles that take the same time.  By a whole wave; in all lanes.
+__device__ inline int64_t first_tile_of_xcd(const int *__restrict__ offsets, int E, int64_t R, int64_t each, int x) {
+    constexpr int START = 256;
+    if (x == 8) return E * each;
+    const int lane = threadIdx.x & 63;
+    auto time_of = [&](int e) -> int64_t {
+        if (e >= E) return 0;
+        int64_t lo, hi;
+        expert_rows(offsets, E, R, e, lo, hi);
+        return hi - lo + START;
+    };
+    int64_t total = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+        int64_t t = time_of(e0 + lane);
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d);
+        total += t;
+    }
+    int64_t target = total * x / 8;
+    for (int e0 = 0;; e0 += 64) {
+        const int64_t t = time_of(e0 + lane);
+        int64_t upto = t;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t up = __shfl_up(upto, d);
+            if (lane >= d) upto += up;
+        }
+        const uint64_t past = __ballot(upto > target);            // the expert: the first of these
+        if (past == 0 && e0 + 64 < E) {
+            target -= __shfl(upto, 63);
+            continue;
+        }
+        const int at = past == 0 ? 63 : __ffsll((unsigned long long)past) - 1;
+        const int64_t before = __shfl(upto - t, at), own = __shfl(t, at);
+        const int64_t tile = (e0 + at) * each + (own > 0 ? (target - before) * each / own : 0);
+        return tile < E * each ? tile : E * each;
+    }
+}
+
 // Blocks of at most `rows` rows of one expert: at most this many.
 inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
     return R / rows + (E + 1 < R ? E + 1 : R);
