@@ -223,7 +223,7 @@ int emu_set_sgemm_split(int mode);
    outputs NaN).  They raise no EMU_STATUS_* bits.
    Matrices are row-major with leading dimensions in elements, at any element's
    alignment; index arrays are int32.  Device pointers, ordered on the current
-   stream, no host synchronisation.  The workspace is used by emu_moe_route
+   stream, no host synchronisation (but where the workspace grows).  It is used by emu_moe_route
    (more than 64 tokens), emu_q4_gemm (a reduction that is split) and the
    grouped products (16-bit operands that are copied to 16-byte alignment first,
    sums of few matrices in pieces); the last three do without it where it cannot
@@ -317,7 +317,8 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
    queued on the previous one (an event dependency, no host synchronisation),
    since every call uses the one workspace; not so a stream under capture,
    where the caller orders the graph's launches.  A captured call must find the
-   workspace grown already (by the same call before the capture).  EMU_OK, or
+   workspace grown already (by the same call before the capture), and its graph
+   is good until the workspace grows again or is released.  EMU_OK, or
    EMU_EHIP if the event calls fail. */
 int emu_set_stream(void *hip_stream);
 

@@ -320,8 +320,9 @@ def _ptr(t):
 
 def _launch(fn, device, *args):
     """One call on the current stream of the operands' device."""
-    if device.index == torch.cuda.current_device():
-        _bind_stream(device)
+    at = device.index
+    if at == torch._C._cuda_getDevice():
+        lib().emu_set_stream(torch._C._cuda_getCurrentRawStream(at))
         rc = fn(*args)
     else:
         with torch.cuda.device(device):
@@ -334,6 +335,13 @@ def _launch(fn, device, *args):
 def _same_gpu(*named):
     """Every tensor that is given is on the first one's GPU."""
     first, lead = named[0]
+    at = lead.get_device()                      # (device objects cost more to compare)
+    for _, t in named:
+        if t is not None and t.get_device() != at:
+            break
+    else:
+        if at >= 0:
+            return
     device = lead.device
     for name, t in named:
         if t is None:
@@ -357,10 +365,10 @@ def moe_route(logits: torch.Tensor, k: int, scope: str = "chosen") -> Routing:
     T, E = logits.shape
     _same_gpu(("logits", logits))
     dev = logits.device
-    ids, slots = logits.new_empty((T, k), dtype=torch.int32), logits.new_empty((T, k), dtype=torch.int32)
-    rows = logits.new_empty(T * k, dtype=torch.int32)
+    # one allocation for four (1.5 us each)
+    ids, slots, rows, weights = logits.new_empty((4, T, k), dtype=torch.int32).unbind(0)
+    rows, weights = rows.view(-1), weights.view(torch.float32)
     offsets = logits.new_empty(E + 1, dtype=torch.int32)
-    weights = logits.new_empty((T, k), dtype=torch.float32)
     _launch(lib().emu_moe_route, dev, code, T, E, k, how, logits.data_ptr(), _ld(logits),
             ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
             slots.data_ptr())
