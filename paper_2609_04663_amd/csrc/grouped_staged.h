@@ -17,8 +17,8 @@
 // flushed per panel of 256: 16 exact products are added per rounding, so even at
 // K = 8192 the 512 roundings of a sum stay below those of a plain FP32 product.
 //
-// Bytes in LDS per k-block of FP32 at 256 x 128: 74 KB written, 196 KB read in the
-// 3072 cycles of its MFMAs, so the matrix instructions bound it: 8192 x 8192 x
+// Bytes in LDS per k-block of FP32 at 256 x 128: 74 KB written, 196 KB read while
+// its MFMAs take 3.1 thousand cycles, so the matrix instructions bound it: 8192 x 8192 x
 // 8192 in one expert takes 5.1 to 5.7 ms (193 to 214 TFLOP/s), the library's SGEMM
 // with its split pass 5.2.
 #pragma once

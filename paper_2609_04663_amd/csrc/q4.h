@@ -23,7 +23,7 @@
 //     in a second buffer where it does not fit at once; a fragment is put into the
 //     fields' order after it is read, and one more matrix instruction with ones
 //     gives the sums.  16 rows of 16384 x 16384: 63 us, prepared 84; one row of
-//     64 matrices of 4096 x 4096: 136 us, prepared 118.
+//     64 matrices of 4096 x 4096: 136 us, prepared 116.
 // The waves of a workgroup share the reduction (and the columns, where x leaves
 // room for few indices only) and add up their sums in LDS at the end.
 #pragma once
@@ -62,17 +62,24 @@ __device__ __forceinline__ f32x4 mfma16(frag<half> a, frag<half> b, f32x4 c) {
 
 // 16 + q of the eight 4-bit fields of w, fields (0, 4), (1, 5), (2, 6), (3, 7)
 // in the pairs of the result.  16 is 0x4180 in bfloat16 (field at bit 3) and
-// 0x4C00 in half (field at bit 6).
+// 0x4C00 in half (field at bit 6).  The mask comes in a register, so that a shift and one
+// v_and_or_b32 make a pair (two constants would be two instructions).
 template <typename C>
-__device__ __forceinline__ frag<C> sixteen_plus(unsigned w) {
+__device__ __forceinline__ unsigned field_mask() {
+    unsigned m = std::is_same<C, bhalf>::value ? 0x00780078u : 0x03C003C0u;
+    asm("" : "+v"(m));
+    return m;
+}
+template <typename C>
+__device__ __forceinline__ frag<C> sixteen_plus(unsigned w, unsigned mask) {
     constexpr bool BF = std::is_same<C, bhalf>::value;
-    constexpr unsigned MASK = BF ? 0x00780078u : 0x03C003C0u, ONE = BF ? 0x41804180u : 0x4C004C00u;
+    constexpr unsigned ONE = BF ? 0x41804180u : 0x4C004C00u;
     constexpr int UP = BF ? 3 : 6;
     u32x4 r;
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
         const unsigned v = 4 * p < UP ? w << (UP - 4 * p) : w >> (4 * p - UP);
-        r[p] = (v & MASK) | ONE;
+        r[p] = (v & mask) | ONE;
     }
     return __builtin_bit_cast(frag<C>, r);
 }
@@ -320,6 +327,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             x.s[i] = load_groups(s_row[i], b);
+            x.o[i] = vec<T, U * GB>{};
             if (g.mins) x.o[i] = load_groups(m_row[i], b);
         }
     };
@@ -332,6 +340,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
 #pragma unroll
         for (int j = 0; j < 4; ++j) at[a][j] = place(0, tok, 4 * j + h);
     }
+    const unsigned mask = field_mask<C>();
     frag<C> ones;
 #pragma unroll
     for (int i = 0; i < 8; ++i) ones[i] = (C)1.0f;
@@ -419,7 +428,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
                     }
 #pragma unroll
                     for (int i = 0; i < NT; ++i) {
-                        const frag<C> wf = sixteen_plus<C>(w[i][j]);
+                        const frag<C> wf = sixteen_plus<C>(w[i][j], mask);
 #pragma unroll
                         for (int c = PL - 1; c >= 0; --c)
 #pragma unroll
@@ -430,26 +439,26 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
                     if ((32 * j + 32) % G == 0) {
 #pragma unroll
                         for (int i = 0; i < NT; ++i) {
-                            const float s = (float)now.s[i][u * GB + 32 * j / G];
+                            const float s = (float)now.s[i][u * GB + 32 * j / G], o = (float)now.o[i][u * GB + 32 * j / G];
+                            if constexpr (RAW) {      // s acc + (start s + offset) sum x
+                                const float e = fmaf(start, s, o);
 #pragma unroll
-                            for (int a = 0; a < MT; ++a)
+                                for (int a = 0; a < MT; ++a)
 #pragma unroll
-                                for (int r = 0; r < REGS; ++r) {
-                                    float v = acc[i][a][r];
-                                    if constexpr (RAW) v = fmaf(xs[a][r], start, v);
-                                    y[i][a][r] = fmaf(v, s, y[i][a][r]);
-                                }
-                            if (g.mins) {
-                                const float o = (float)now.o[i][u * GB + 32 * j / G] * (RAW ? 1.0f : 1.0f / -16.0f);    // of start
+                                    for (int r = 0; r < REGS; ++r)
+                                        y[i][a][r] = fmaf(xs[a][r], e, fmaf(acc[i][a][r], s, y[i][a][r]));
+                            } else {                  // the sums are start sum x, and in acc
 #pragma unroll
-                                for (int a = 0; a < MT; ++a) {
-                                    if constexpr (!RAW) {
+                                for (int a = 0; a < MT; ++a)
+#pragma unroll
+                                    for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(acc[i][a][r], s, y[i][a][r]);
+                                if (g.mins) {
+#pragma unroll
+                                    for (int a = 0; a < MT; ++a) {
                                         const sums_t v = *reinterpret_cast<const sums_t *>(sum + 16 * a);
 #pragma unroll
-                                        for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(v[r], o, y[i][a][r]);
-                                    } else {
-#pragma unroll
-                                        for (int r = 0; r < REGS; ++r) y[i][a][r] = fmaf(xs[a][r], o, y[i][a][r]);
+                                        for (int r = 0; r < REGS; ++r)
+                                            y[i][a][r] = fmaf(v[r], o * (1.0f / -16.0f), y[i][a][r]);
                                     }
                                 }
                             }
@@ -600,14 +609,17 @@ hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
         const integral_constant<int, 2> two;
         const integral_constant<int, 3> three;
         const integral_constant<int, 4> four;
-        // A wave has 4 KB of weights in flight, 2 KB where FP32 leaves no registers for
-        // more.  Above 48 FP32 rows tiles of 32, whose weights are read twice: 64 rows of
+        // A wave has 4 KB of weights in flight, 2 KB where the accumulators leave no
+        // registers for more (float32, and tiles of 64).  Two column tiles to a wave above
+        // 16 rows: with four, 40 half rows of 8192 x 8192 took 64 us instead of 40 (spills).
+        // Above 48 float32 rows tiles of 32, whose weights are read twice: 64 rows of
         // 4096 x 8192 take 40 us, a tile of 64, which spills, 95.
         constexpr bool wide = Q4Elem<T>::PLANES == 3;
+        const integral_constant<int, wide ? 1 : 2> set;
         if (g.R <= 16 * (int64_t)g.E) run(one, one, four, group);
-        else if (g.R <= 32 * (int64_t)g.E) run(two, integral_constant<int, wide ? 2 : 4>{}, one, group);
-        else if (g.R <= 48 * (int64_t)g.E) run(three, integral_constant<int, wide ? 2 : 4>{}, one, group);
-        else run(integral_constant<int, wide ? 2 : 4>{}, two, integral_constant<int, wide ? 1 : 2>{}, group);
+        else if (g.R <= 32 * (int64_t)g.E) run(two, two, set, group);
+        else if (g.R <= 48 * (int64_t)g.E) run(three, two, set, group);
+        else run(integral_constant<int, wide ? 2 : 4>{}, two, one, group);
     };
     if (g.group == 32) rows(std::integral_constant<int, 32>{});
     else if (g.group == 64) rows(std::integral_constant<int, 64>{});
