@@ -15,8 +15,8 @@
 // stable order that no atomic decides: a workgroup of 64 tokens sets one bit
 // per token in a 64-bit mask of each expert, so a row's rank among its expert's
 // rows of the workgroup is a population count.  Up to 64 tokens that is the whole order, and
-// one launch does everything.  Beyond, the workgroups' counts are summed up by a second
-// kernel, and a third adds the ranks.
+// one launch does everything.  Beyond, a second kernel adds up the workgroups' counts
+// and ranks the rows; of many counts a kernel of its own makes the sums first.
 //
 // Measured: one token, 64 experts, 8 choices: 4.2 us, of which the launch is most.
 // 16384 tokens in bfloat16, 128 experts, 8 choices: 9.5 + 4 + 4 us, the gradient 5.4;
@@ -29,6 +29,9 @@ namespace emu {
 namespace {
 
 constexpr int TOKENS = 64;          // tokens of a workgroup
+
+// Entries of a row of counts: 16-byte loads, the entries past E are zeros.
+__host__ __device__ constexpr int padded(int E) { return (E + 3) & ~3; }
 
 // Unsigned order of floats: larger value, larger number; -inf and NaN give 0.
 __device__ __forceinline__ unsigned ordered(float x) {
@@ -58,15 +61,23 @@ __device__ __forceinline__ T over_lanes(T v, F f) {
     return v;
 }
 
+// Bits of a logit in bfloat16 or binary16 as a float that are zero in either.
+constexpr unsigned INDEX = (1u << 13) - 1;
+
 // One token's choice by LANES lanes that hold the logits lane + LANES i in
 // x[i] (-inf past E).  Lane j % LANES of the group keeps choice j in slot
 // j / LANES of id and w; returns in *live how many were chosen.
-template <int LANES, int V>
+// PACKED (16-bit logits): their ordered bits are those above INDEX, where the expert's
+// number goes, so that one exchange finds the largest logit and its lowest index.
+template <int LANES, int V, bool PACKED>
 __device__ __forceinline__ void choose(const float (&x)[V], int sub, int k, bool all,
                                        int (&id)[ROUTE_CHOICES / 16], float (&w)[ROUTE_CHOICES / 16]) {
     unsigned o[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = ordered(x[i]);
+    for (int i = 0; i < V; ++i) {
+        o[i] = ordered(x[i]);
+        if constexpr (PACKED) o[i] = o[i] == 0 ? 0u : (o[i] | INDEX) - (sub + LANES * i);
+    }
     constexpr int SLOTS = ROUTE_CHOICES / 16;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s) {
@@ -81,11 +92,18 @@ __device__ __forceinline__ void choose(const float (&x)[V], int sub, int k, bool
         best = over_lanes<LANES>(best, [](unsigned a, unsigned b) { return a > b ? a : b; });
         if (best == 0) break;                                 // no expert is left
         int at = 0x7FFFFFFF;
+        if constexpr (PACKED) {
+            at = INDEX - (best & INDEX);
 #pragma unroll
-        for (int i = V - 1; i >= 0; --i) at = o[i] == best ? sub + LANES * i : at;
-        at = over_lanes<LANES>(at, [](int a, int b) { return a < b ? a : b; });
+            for (int i = 0; i < V; ++i) o[i] = o[i] == best ? 0u : o[i];
+            best = best & 0x80000000u ? best & ~INDEX : best | INDEX;
+        } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) o[i] = at == sub + LANES * i ? 0u : o[i];
+            for (int i = V - 1; i >= 0; --i) at = o[i] == best ? sub + LANES * i : at;
+            at = over_lanes<LANES>(at, [](int a, int b) { return a < b ? a : b; });
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[i] = at == sub + LANES * i ? 0u : o[i];
+        }
         const float v = unordered(best);
         if (j == 0) m = v;
 #pragma unroll
@@ -146,8 +164,8 @@ __global__ __launch_bounds__(1024) void route_kernel(const T *__restrict__ logit
                                                      int *__restrict__ rows, int *__restrict__ slots) {
     __shared__ unsigned long long mask[ROUTE_EXPERTS];
     __shared__ int start[ROUTE_EXPERTS], part[16];
-    const int tid = threadIdx.x, sub = tid % LANES;
-    if (tid < E) mask[tid] = 0;
+    const int tid = threadIdx.x, sub = tid % LANES, lde = padded(E);
+    if (tid < lde) mask[tid] = 0;
     __syncthreads();
     constexpr int AT_ONCE = 1024 / LANES;
     const bool single = gridDim.x == 1;
@@ -159,7 +177,7 @@ __global__ __launch_bounds__(1024) void route_kernel(const T *__restrict__ logit
         const bool live = t < tokens;
         float x[V], w[ROUTE_CHOICES / 16];
         load_logits<LANES, V>(logits + (live ? t : 0) * ld, E, sub, live, x);
-        choose<LANES, V>(x, sub, k, all, id[p], w);
+        choose<LANES, V, sizeof(T) == 2>(x, sub, k, all, id[p], w);
 #pragma unroll
         for (int s = 0; s < ROUTE_CHOICES / 16; ++s) {
             const int j = sub + LANES * s;
@@ -171,8 +189,7 @@ __global__ __launch_bounds__(1024) void route_kernel(const T *__restrict__ logit
     }
     __syncthreads();
     if (!single) {
-        for (int e = tid; e < E; e += 1024)
-            counts[(int64_t)blockIdx.x * E + e] = __popcll(mask[e]);
+        if (tid < lde) counts[(int64_t)blockIdx.x * lde + tid] = __popcll(mask[tid]);
         return;
     }
     int total;
@@ -204,44 +221,75 @@ __global__ __launch_bounds__(1024) void route_kernel(const T *__restrict__ logit
 __global__ __launch_bounds__(64) void route_sums_kernel(int *__restrict__ counts, int64_t blocks,
                                                         int E, int *__restrict__ totals) {
     constexpr int AHEAD = 4;
-    const int lane = threadIdx.x, e = blockIdx.x;
+    const int lane = threadIdx.x, e = blockIdx.x, lde = padded(E);
     int before = 0;
     for (int64_t b0 = lane; b0 - lane < blocks; b0 += 64 * AHEAD) {
         int n[AHEAD];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) n[i] = b0 + 64 * i < blocks ? counts[(b0 + 64 * i) * E + e] : 0;
+        for (int i = 0; i < AHEAD; ++i) n[i] = b0 + 64 * i < blocks ? counts[(b0 + 64 * i) * lde + e] : 0;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int v = sum_up_to_lane(n[i]);
-            if (b0 + 64 * i < blocks) counts[(b0 + 64 * i) * E + e] = before + v - n[i];
+            if (b0 + 64 * i < blocks) counts[(b0 + 64 * i) * lde + e] = before + v - n[i];
             before += __builtin_amdgcn_readlane(v, 63);
         }
     }
     if (lane == 0) totals[e] = before;
 }
 
-// Slots and rows of 64 tokens, from their experts and the sums of the counts.
+// Slots and rows of 64 tokens, from their experts and the counts: as route_sums_kernel
+// left them, or (ADD) as route_kernel did, where every workgroup adds up those of
+// all, a quad of experts and every 1024 / quads-th row to a thread.
+template <bool ADD>
 __global__ __launch_bounds__(1024) void route_order_kernel(const int *__restrict__ ids, int64_t tokens,
                                                            int E, int k, const int *__restrict__ counts,
-                                                           const int *__restrict__ totals,
+                                                           int blocks, const int *__restrict__ totals,
                                                            int *__restrict__ offsets,
                                                            int *__restrict__ rows,
                                                            int *__restrict__ slots) {
     __shared__ unsigned long long mask[ROUTE_EXPERTS];
-    __shared__ int start[ROUTE_EXPERTS], part[16];
-    const int tid = threadIdx.x;
+    __shared__ int start[ROUTE_EXPERTS], every[ADD ? ROUTE_EXPERTS : 1], part[16];
+    const int tid = threadIdx.x, lde = padded(E);
     const int64_t t0 = (int64_t)blockIdx.x * TOKENS;
     const int n = (int)((tokens - t0 < TOKENS ? tokens - t0 : TOKENS) * k);
-    if (tid < E) mask[tid] = 0;
+    if (tid < lde) {
+        mask[tid] = 0;
+        if constexpr (ADD) start[tid] = every[tid] = 0;
+    }
     __syncthreads();
     for (int i = tid; i < n; i += 1024) {
         const int e = ids[t0 * k + i];
         if (e >= 0) atomicOr(&mask[e], 1ull << (i / k));
     }
+    if constexpr (ADD) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        constexpr int AHEAD = 8;
+        const int quads = lde / 4, at_once = 1024 / quads, q = tid % quads, first = tid / quads;
+        i32x4 before = {}, all = {};
+        for (int b0 = first; first < at_once && b0 < blocks; b0 += at_once * AHEAD) {
+            i32x4 c[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                const int b = b0 + at_once * i;
+                c[i] = b < blocks ? reinterpret_cast<const i32x4 *>(counts + (int64_t)b * lde)[q] : i32x4{};
+            }
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                all += c[i];
+                if (b0 + at_once * i < (int)blockIdx.x) before += c[i];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {                         // whole numbers: any order
+            if (all[j] != 0) atomicAdd(&every[4 * q + j], all[j]);
+            if (before[j] != 0) atomicAdd(&start[4 * q + j], before[j]);
+        }
+        __syncthreads();
+    }
     int total;
-    const int below = sums_below(E, [&](int e) { return totals[e]; }, part, &total);
+    const int below = sums_below(E, [&](int e) { return ADD ? every[e] : totals[e]; }, part, &total);
     if (tid < E) {
-        start[tid] = below + counts[(int64_t)blockIdx.x * E + tid];
+        start[tid] = below + (ADD ? start[tid] : counts[(int64_t)blockIdx.x * lde + tid]);
         if (blockIdx.x == 0) offsets[tid] = below;
     }
     if (blockIdx.x == 0 && tid == 0) offsets[E] = total;
@@ -323,23 +371,29 @@ void with_shape(int E, F &&f) {
     if (E <= 64) f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
     else if (E <= 128) f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
     else if (E <= 256) f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    else if (E <= 512) f(integral_constant<int, 16>{}, integral_constant<int, 32>{});
     else f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
 
+// Counts up to which every workgroup of the order adds them up itself.  With k = 8, the
+// router's time with and without route_sums_kernel, us: 1024 tokens and 128 experts
+// 11.6 and 10.2, 16384 and 128 13.1 and 12.3, 16384 and 256 16.6 and 16.8, 65536 and 64
+// 25.2 and 28.7.
+constexpr int64_t MOST_ADDED = 1 << 15;
 int64_t route_blocks(int64_t T) { return T > TOKENS ? (T + TOKENS - 1) / TOKENS : 1; }
 
 }  // namespace
 
 size_t route_scratch(int64_t T, int E) {
     const int64_t b = route_blocks(T);
-    return b > 1 ? (size_t)(b + 1) * E * sizeof(int) : 0;
+    return b > 1 ? (size_t)(b + 1) * padded(E) * sizeof(int) : 0;
 }
 
 hipError_t launch_route(int dtype, const void *logits, int64_t ld, int64_t T, int E, int k, bool all,
                         int *ids, float *weights, int *offsets, int *rows, int *slots, char *scratch,
                         hipStream_t s) {
     const int64_t blocks = route_blocks(T);
-    int *const counts = reinterpret_cast<int *>(scratch), *const totals = counts + blocks * E;
+    int *const counts = reinterpret_cast<int *>(scratch), *const totals = counts + blocks * padded(E);
     with_type(dtype, [&](auto z) {
         using type = decltype(z);
         with_shape(E, [&](auto lanes, auto v) {
@@ -350,11 +404,14 @@ hipError_t launch_route(int dtype, const void *logits, int64_t ld, int64_t T, in
     });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || blocks == 1) return e;
-    route_sums_kernel<<<E, 64, 0, s>>>(counts, blocks, E, totals);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    route_order_kernel<<<(unsigned)blocks, 1024, 0, s>>>(ids, T, E, k, counts, totals, offsets, rows,
-                                                         slots);
+    const bool add = blocks * padded(E) <= MOST_ADDED;
+    if (!add) {
+        route_sums_kernel<<<E, 64, 0, s>>>(counts, blocks, E, totals);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    (add ? route_order_kernel<true> : route_order_kernel<false>)<<<(unsigned)blocks, 1024, 0, s>>>(
+        ids, T, E, k, counts, (int)blocks, totals, offsets, rows, slots);
     return hipGetLastError();
 }
 
