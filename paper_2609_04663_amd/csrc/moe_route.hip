@@ -5,11 +5,13 @@
 // index of equal ones first; -inf and NaN are never chosen.  With m the largest
 // logit, weights_j = exp(l_j - m) / sum exp(l - m), the sum over the chosen
 // experts or over all (a largest logit of +inf shares the weight among the
-// experts that have it).  Sixteen lanes hold a token's logits in registers, 16
-// values each at most (64 lanes above 256 experts); a round takes the largest
-// ordered bit pattern of the lanes, then the lowest index that has it, each four
-// moves between registers (through LDS they took 2 us more of a launch).  k rounds
-// cost about 40 instructions each for four tokens at once.
+// experts that have it).  Sixteen lanes hold a token's logits in registers, 32
+// values each at most (64 lanes above 512 experts: 16 lanes take a quarter of the
+// instructions, 4096 tokens and 512 experts 42 us with 64 lanes and 21 with 16); a round
+// takes the largest ordered bit pattern of the lanes, then the lowest index that has
+// it, each four moves between registers (through LDS they took 2 us more of a launch).
+// Logits of 16 bits leave room for the index in the pattern, and one exchange does.  k
+// rounds cost 25 to 40 instructions each for four tokens at once.
 //
 // Order.  Rows are ordered by expert, then token (a token's experts differ), a
 // stable order that no atomic decides: a workgroup of 64 tokens sets one bit
@@ -19,9 +21,9 @@
 // and ranks the rows; of many counts a kernel of its own makes the sums first.
 //
 // Measured: one token, 64 experts, 8 choices: 4.2 us, of which the launch is most.
-// 16384 tokens in bfloat16, 128 experts, 8 choices: 9.5 + 4 + 4 us, the gradient 5.4;
-// the bytes alone (4 MB of logits, 2 MB of results) would take 1.5 us, the rest is
-// the launches and the latency of loads that wait for one another.
+// 16384 tokens in bfloat16, 128 experts, 8 choices: 7.3 + 5.6 us (11.7 together in a row
+// of calls), the gradient 5.4; the bytes alone (4 MB of logits, 2 MB of results) would
+// take 1.5 us, the rest is the launches and the latency of loads that wait for one another.
 #include "moe.h"
 #include "moe_common.h"
 
