@@ -315,11 +315,15 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
 /* Stream for subsequent calls (a hipStream_t); NULL selects the default
    stream.  Switching streams orders the new stream after the work already
    queued on the previous one (an event dependency, no host synchronisation),
-   since every call uses the one workspace; not so a stream under capture,
-   where the caller orders the graph's launches.  A captured call must find the
-   workspace grown already (by the same call before the capture), and its graph
-   is good until the workspace grows again or is released.  EMU_OK, or
-   EMU_EHIP if the event calls fail. */
+   since every call uses the one workspace.  Streams under one capture are ordered
+   in the same way, by an edge of its graph (of two captures at a time, the calls
+   of each have to be on one stream).  A graph and what is outside of it are
+   not: the caller orders the graph's launches, and calls outside follow the last
+   ones outside.  A captured call must find the workspace grown already (by the
+   same call before the capture), and its graph is good until the workspace grows
+   again or is released.  EMU_OK, or EMU_EHIP (the stream remains what it was) if
+   a HIP call fails, or if the new stream is not under capture and would have to
+   follow earlier work on one that now is. */
 int emu_set_stream(void *hip_stream);
 
 /* Projection constant of the FP64 split for subsequent emu_dgemm and

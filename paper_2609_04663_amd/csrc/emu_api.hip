@@ -45,7 +45,14 @@ namespace {
 using namespace emu;
 
 hipStream_t g_stream = nullptr;
-hipEvent_t g_switch_event = nullptr;   // orders a new stream after the previous one
+// The streams whose calls the next one on another stream must follow, since all
+// share the workspace: the last one outside of a capture, and the last one of the
+// last capture (an edge of its graph); what orders a graph and the rest is the
+// caller's.  An event for either.
+hipStream_t g_outside = nullptr, g_inside = nullptr;
+unsigned long long g_capture = 0;      // the capture of g_inside; 0: none yet
+bool g_captured = false;               // g_stream was under capture when it was set
+hipEvent_t g_outside_event = nullptr, g_inside_event = nullptr;
 int g_split_mode = EMU_SPLIT_SYM;
 int g_split_scope = EMU_SCOPE_OPERAND;
 int g_fallback = EMU_FALLBACK_NONE;
@@ -72,6 +79,7 @@ int fail(int code, const char *msg) {
 
 int hip_fail(hipError_t e, const char *what) {
     g_err = std::string(what) + ": " + hipGetErrorString(e);
+    (void)hipGetLastError();            // reported here, and not by the next launch again
     return EMU_EHIP;
 }
 
@@ -81,7 +89,65 @@ size_t workspace_limit() {
     return (size_t)strtoull(s, nullptr, 0);
 }
 
+// The capture that a stream is under, 0 for none.
+int capture_of(hipStream_t s, unsigned long long *id) {
+    *id = 0;
+    if (s == nullptr) return EMU_OK;    // (the default stream cannot be captured)
+    hipStreamCaptureStatus state = hipStreamCaptureStatusNone;
+    const hipError_t e = hipStreamGetCaptureInfo(s, &state, id);
+    if (e != hipSuccess) return hip_fail(e, "hipStreamGetCaptureInfo");
+    if (state == hipStreamCaptureStatusNone) *id = 0;
+    return EMU_OK;
+}
+
+// What is queued on `s` from now on follows what `before` holds (inside of a
+// capture an edge of the graph).  No host synchronisation.
+int follow(hipStream_t s, hipStream_t before, hipEvent_t *event) {
+    hipError_t e = hipSuccess;
+    if (!*event) e = hipEventCreateWithFlags(event, hipEventDisableTiming);
+    if (e != hipSuccess) {
+        *event = nullptr;
+        return hip_fail(e, "hipEventCreateWithFlags");
+    }
+    e = hipEventRecord(*event, before);
+    if (e == hipSuccess) e = hipStreamWaitEvent(s, *event, 0);
+    return e == hipSuccess ? EMU_OK : hip_fail(e, "stream switch");
+}
+
+int switch_stream(hipStream_t s) {
+    unsigned long long was = 0, now = 0;
+    if (int rc = capture_of(g_stream, &was)) return rc;
+    if (int rc = capture_of(s, &now)) return rc;
+    if (was != 0) {                     // it may have begun since the stream was set
+        g_inside = g_stream;
+        g_capture = was;
+    }
+    if (now != 0) {
+        if (g_ws.base && g_capture == now && g_inside != s)
+            if (int rc = follow(s, g_inside, &g_inside_event)) return rc;
+        g_inside = s;
+        g_capture = now;
+    } else {
+        if (g_ws.base && g_outside != s) {
+            // an event recorded on a stream under capture would draw `s` into it
+            if (int rc = capture_of(g_outside, &was)) return rc;
+            if (was != 0) return fail(EMU_EHIP, "stream switch: the previous stream is under capture");
+            if (int rc = follow(s, g_outside, &g_outside_event)) return rc;
+        }
+        g_outside = s;
+    }
+    g_stream = s;
+    g_captured = now != 0;
+    return EMU_OK;
+}
+
 int ensure_workspace(size_t need) {
+    if (g_captured) {                   // the capture may have ended: calls outside of it follow one another
+        unsigned long long id = 0;
+        if (int rc = capture_of(g_stream, &id)) return rc;
+        if (id == 0)
+            if (int rc = switch_stream(g_stream)) return rc;
+    }
     need += HDR;
     if (need <= g_ws.bytes) return EMU_OK;
     if (need > workspace_limit()) return fail(EMU_ENOMEM, "workspace would exceed EMU_WORKSPACE_LIMIT");
@@ -276,32 +342,7 @@ extern "C" {
 
 int emu_set_stream(void *hip_stream) {
     const hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-    bool capturing = false;
-    if (s != g_stream && s != nullptr) {
-        hipStreamCaptureStatus state = hipStreamCaptureStatusNone;
-        const hipError_t e = hipStreamIsCapturing(s, &state);
-        if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
-        capturing = state == hipStreamCaptureStatusActive;
-    }
-    if (s != g_stream && g_ws.base && !capturing) {
-        // Every call shares the one workspace: work queued on the new stream
-        // must not start before the calls already queued on the old one are
-        // done with it.  An event dependency, no host synchronisation.  (A
-        // stream under capture runs nothing now and cannot wait for outside
-        // work; whoever launches the graph orders it.)
-        if (!g_switch_event) {
-            hipError_t e = hipEventCreateWithFlags(&g_switch_event, hipEventDisableTiming);
-            if (e != hipSuccess) {
-                g_switch_event = nullptr;
-                return hip_fail(e, "hipEventCreateWithFlags");
-            }
-        }
-        hipError_t e = hipEventRecord(g_switch_event, g_stream);
-        if (e == hipSuccess) e = hipStreamWaitEvent(s, g_switch_event, 0);
-        if (e != hipSuccess) return hip_fail(e, "stream switch");
-    }
-    g_stream = s;
-    return EMU_OK;
+    return s == g_stream && !g_captured ? EMU_OK : switch_stream(s);
 }
 
 int emu_set_split_mode(int mode) {
