@@ -130,7 +130,7 @@ def _check(rc: int):
 
 def _bind_stream(dev: torch.device):
     # the handle alone: a torch.cuda.Stream object costs 2 us to make
-    lib().emu_set_stream(torch._C._cuda_getCurrentRawStream(dev.index))
+    _check(lib().emu_set_stream(torch._C._cuda_getCurrentRawStream(dev.index)))
 
 
 def _layout(t: torch.Tensor, dtype, name: str):
@@ -322,8 +322,9 @@ def _launch(fn, device, *args):
     """One call on the current stream of the operands' device."""
     at = device.index
     if at == torch._C._cuda_getDevice():
-        lib().emu_set_stream(torch._C._cuda_getCurrentRawStream(at))
-        rc = fn(*args)
+        rc = lib().emu_set_stream(torch._C._cuda_getCurrentRawStream(at))
+        if rc == EMU_OK:
+            rc = fn(*args)
     else:
         with torch.cuda.device(device):
             _bind_stream(device)
