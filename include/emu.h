@@ -227,7 +227,7 @@ int emu_set_sgemm_split(int mode);
    (more than 64 tokens), emu_q4_gemm (a reduction that is split) and the
    grouped products (16-bit operands that are copied to 16-byte alignment first,
    sums of few matrices in pieces); the last three do without it where it cannot
-   grow.
+   grow (no memory beside what is held, EMU_WORKSPACE_LIMIT, a stream under capture).
    offsets: E + 1 entries, rows [offsets[e], offsets[e + 1]) belong to expert e
    (offsets[0] counts as 0); an expert may have none.  Rows from offsets[E] on
    belong to no expert: their outputs are zero and their inputs are not used.
@@ -320,8 +320,8 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
    of each have to be on one stream).  A graph and what is outside of it are
    not: the caller orders the graph's launches, and calls outside follow the last
    ones outside.  A captured call must find the workspace grown already (by the
-   same call before the capture), and its graph is good until the workspace grows
-   again or is released.  EMU_OK, or EMU_EHIP (the stream remains what it was) if
+   same call before the capture; else EMU_ENOMEM, or it does without), and its
+   graph is good until the workspace grows again or is released.  EMU_OK, or EMU_EHIP (the stream remains what it was) if
    a HIP call fails, or if the new stream is not under capture and would have to
    follow earlier work on one that now is. */
 int emu_set_stream(void *hip_stream);

@@ -65,7 +65,8 @@ std::string g_err;
 struct Workspace {
     char *base = nullptr;
     size_t bytes = 0;
-    size_t refused = (size_t)-1;   // smallest size that the device could not give
+    size_t refused = (size_t)-1;   // smallest size that the device could not give,
+    size_t refused_beside = (size_t)-1;    // and the same beside what is held now
     unsigned status = 0;           // the status word while nothing is held after a refusal
 } g_ws;
 
@@ -141,27 +142,59 @@ int switch_stream(hipStream_t s) {
     return EMU_OK;
 }
 
+// A call that uses the workspace on the current stream: whether that is under capture.
+// Where its capture has ended since it was set, the call follows those outside.
+int workspace_user(bool *capturing) {
+    unsigned long long id = 0;
+    if (int rc = capture_of(g_stream, &id)) return rc;
+    *capturing = id != 0;
+    return g_captured && id == 0 ? switch_stream(g_stream) : EMU_OK;
+}
+
+// The status word of the held workspace, when its calls are done.
+int held_status(unsigned *status) {
+    *status = g_ws.status;
+    if (!g_ws.base) return EMU_OK;
+    hipError_t e = hipStreamSynchronize(g_stream);
+    if (e != hipSuccess) return hip_fail(e, "hipStreamSynchronize");
+    e = hipMemcpy(status, g_ws.base, sizeof(*status), hipMemcpyDeviceToHost);
+    return e == hipSuccess ? EMU_OK : hip_fail(e, "hipMemcpy(status)");
+}
+
+int free_held() {
+    if (!g_ws.base) return EMU_OK;
+    const hipError_t e = hipFree(g_ws.base);
+    g_ws.base = nullptr;
+    g_ws.bytes = 0;
+    g_ws.refused_beside = (size_t)-1;
+    return e == hipSuccess ? EMU_OK : hip_fail(e, "hipFree");
+}
+
+// A new workspace: its header.
+int fill_header(void *p, unsigned status) {
+    hipError_t e = hipMemcpy(p, &status, sizeof(status), hipMemcpyHostToDevice);
+    if (e != hipSuccess) return hip_fail(e, "hipMemcpy(status)");
+    e = hipMemset((char *)p + sizeof(status), 0, HDR - sizeof(status));
+    return e == hipSuccess ? EMU_OK : hip_fail(e, "hipMemset(header)");
+}
+
+void hold(void *p, size_t bytes) {
+    g_ws.base = (char *)p;
+    g_ws.bytes = bytes;
+    g_ws.status = 0;
+    g_ws.refused_beside = (size_t)-1;
+}
+
 int ensure_workspace(size_t need) {
-    if (g_captured) {                   // the capture may have ended: calls outside of it follow one another
-        unsigned long long id = 0;
-        if (int rc = capture_of(g_stream, &id)) return rc;
-        if (id == 0)
-            if (int rc = switch_stream(g_stream)) return rc;
-    }
+    bool capturing = false;
+    if (int rc = workspace_user(&capturing)) return rc;
     need += HDR;
     if (need <= g_ws.bytes) return EMU_OK;
+    if (capturing) return fail(EMU_ENOMEM, "the workspace cannot grow while the stream is under capture");
     if (need > workspace_limit()) return fail(EMU_ENOMEM, "workspace would exceed EMU_WORKSPACE_LIMIT");
-    unsigned status = g_ws.status;
-    if (g_ws.base) {
-        hipError_t e = hipStreamSynchronize(g_stream);
-        if (e != hipSuccess) return hip_fail(e, "hipStreamSynchronize");
-        e = hipMemcpy(&status, g_ws.base, sizeof(status), hipMemcpyDeviceToHost);
-        if (e != hipSuccess) return hip_fail(e, "hipMemcpy(status)");
-        e = hipFree(g_ws.base);
-        g_ws.base = nullptr;
-        g_ws.bytes = 0;
-        if (e != hipSuccess) return hip_fail(e, "hipFree");
-    }
+    unsigned status = 0;
+    if (int rc = held_status(&status)) return rc;
+    if (int rc = free_held()) return rc;
     void *p = nullptr;
     hipError_t e = hipMalloc(&p, need);
     if (e != hipSuccess || !p) {
@@ -170,20 +203,47 @@ int ensure_workspace(size_t need) {
         g_ws.status = status;
         return fail(EMU_ENOMEM, "hipMalloc of the workspace failed");
     }
-    e = hipMemcpy(p, &status, sizeof(status), hipMemcpyHostToDevice);
-    if (e != hipSuccess) {
+    if (int rc = fill_header(p, status)) {
         (void)hipFree(p);
-        return hip_fail(e, "hipMemcpy(status)");
+        return rc;
     }
-    e = hipMemset((char *)p + sizeof(status), 0, HDR - sizeof(status));
-    if (e != hipSuccess) {
-        (void)hipFree(p);
-        return hip_fail(e, "hipMemset(header)");
-    }
-    g_ws.base = (char *)p;
-    g_ws.bytes = need;
-    g_ws.status = 0;
+    hold(p, need);
     return EMU_OK;
+}
+
+// The same for a call that can do without: where the larger workspace is not to
+// be had, *there is false and what is held stays where it is.  So the new one is
+// allocated beside the held one, and a size that the device refused is not tried
+// again on every call.
+int try_workspace(size_t need, bool *there) {
+    *there = false;
+    bool capturing = false;
+    if (int rc = workspace_user(&capturing)) return rc;
+    need += HDR;
+    if (need <= g_ws.bytes) {
+        *there = true;
+        return EMU_OK;
+    }
+    if (capturing || need > workspace_limit() || need >= g_ws.refused || need >= g_ws.refused_beside) return EMU_OK;
+    void *p = nullptr;
+    const hipError_t e = hipMalloc(&p, need);
+    if (e == hipErrorOutOfMemory || (e == hipSuccess && !p)) {
+        (void)hipGetLastError();
+        g_ws.refused_beside = need;
+        return EMU_OK;
+    }
+    if (e != hipSuccess) return hip_fail(e, "hipMalloc of the workspace");
+    unsigned status = 0;
+    int rc = held_status(&status);
+    if (rc == EMU_OK) rc = fill_header(p, status);
+    if (rc != EMU_OK) {
+        (void)hipFree(p);
+        return rc;
+    }
+    rc = free_held();
+    hold(p, need);
+    *there = rc == EMU_OK;
+    return rc;
 }
 
 // Grows the workspace for the layout of a depth-d DGEMM and `rest` more bytes.
@@ -336,6 +396,12 @@ int api_workspace(size_t bytes, char **p) {
     if (rc == EMU_OK) *p = g_ws.base + HDR;
     return rc;
 }
+int api_try_workspace(size_t bytes, char **p) {
+    bool there = false;
+    const int rc = try_workspace(bytes > 0 ? bytes : 1, &there);
+    *p = there ? g_ws.base + HDR : nullptr;
+    return rc;
+}
 }  // namespace emu
 
 extern "C" {
@@ -379,16 +445,12 @@ const char *emu_last_error(void) { return g_err.c_str(); }
 int64_t emu_workspace_bytes(void) { return (int64_t)g_ws.bytes; }
 
 int emu_release_workspace(void) {
-    g_ws.refused = (size_t)-1;
+    g_ws.refused = g_ws.refused_beside = (size_t)-1;
     g_ws.status = 0;
     if (!g_ws.base) return EMU_OK;
-    hipError_t e = hipDeviceSynchronize();
+    const hipError_t e = hipDeviceSynchronize();
     if (e != hipSuccess) return hip_fail(e, "hipDeviceSynchronize");
-    e = hipFree(g_ws.base);
-    g_ws.base = nullptr;
-    g_ws.bytes = 0;
-    if (e != hipSuccess) return hip_fail(e, "hipFree");
-    return EMU_OK;
+    return free_held();
 }
 
 int emu_profile_enable(int on) {

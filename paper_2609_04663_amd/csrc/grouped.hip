@@ -125,13 +125,15 @@ static hipError_t run_direct(const GroupedGemm &g, hipStream_t s) {
 }
 
 // A 16-bit product on copies of the operands that the direct kernels cannot take, if
-// that is faster than the kernels of grouped_staged.h; false: nothing was launched.
+// that is faster than the kernels of grouped_staged.h: *done, or else nothing was
+// launched.
 // Those reach 550 TFLOP/s ('N' 330, whose matrix they transpose by narrow loads).  8
 // experts of 2041 x 2041 with 1000 rows in bfloat16 'N': staged 237 us, on copies 109;
 // 64 with 300 rows: 1270 and 462; 8191 x 8191 x 8191 'T': 1341 and 977, the gradient
 // of its matrix 7358 and 1040.
-static bool realigned_gemm(const GroupedGemm &g, hipStream_t s, hipError_t *e) {
-    if (g.dtype == EMU_F32 || g.K == 0 || g.E == 0) return false;
+static int realigned_gemm(const GroupedGemm &g, hipStream_t s, bool *done) {
+    *done = false;
+    if (g.dtype == EMU_F32 || g.K == 0 || g.E == 0) return EMU_OK;
     const int64_t K = g.K <= BK ? 2 * BK : up(g.K, BK), xr = g.rows && g.xrows <= g.R ? g.xrows : g.R;
     const bool pad = K != g.K, x = pad || !aligned16(g.X) || g.ldx % 8;
     const bool w = pad || !aligned16(g.W) || g.ldw % 8 || g.sw % 8 || (!g.transb && g.N % 8);
@@ -144,7 +146,7 @@ static bool realigned_gemm(const GroupedGemm &g, hipStream_t s, hipError_t *e) {
     const int64_t xb = x ? up(cx.bytes(), 256) : 0, wb = w ? cw.bytes() : 0;
     const double work = 2.0 * g.R * g.N * g.K / 1e6;            // operations per us at 1 TFLOP/s
     const double copied = work / 1000 + (x ? copy_time(cx) : 0) + (w ? copy_time(cw) : 0);
-    if (copied >= work / (g.transb ? 550 : 330) || xb + wb > MOST_COPIED) return false;
+    if (copied >= work / (g.transb ? 550 : 330) || xb + wb > MOST_COPIED) return EMU_OK;
     GroupedGemm d = g;
     d.K = (int)K;
     if (x) {
@@ -156,28 +158,34 @@ static bool realigned_gemm(const GroupedGemm &g, hipStream_t s, hipError_t *e) {
         d.ldw = cw.ld;
         d.sw = g.sw == 0 ? 0 : cw.rows * cw.ld;
     }
+    if (x) d.X = nullptr;
+    if (w) d.W = nullptr;
+    if (!direct_gemm(d, w)) return EMU_OK;                      // offsets
     char *at = nullptr;
-    if (api_workspace(xb + wb, &at) != EMU_OK) {
-        api_clear_error();
-        return false;
-    }
+    if (int rc = api_try_workspace(xb + wb, &at)) return rc;
+    if (!at) return EMU_OK;
     if (x) d.X = at;
     if (w) d.W = at + xb;
-    if (!direct_gemm(d, w)) return false;                       // offsets
-    *e = x ? realign(cx, at, s) : hipSuccess;
-    if (*e == hipSuccess && w) *e = realign(cw, at + xb, s);
-    if (*e == hipSuccess) *e = run_direct(d, s);
-    return true;
+    *done = true;
+    hipError_t e = x ? realign(cx, at, s) : hipSuccess;
+    if (e == hipSuccess && w) e = realign(cw, at + xb, s);
+    if (e == hipSuccess) e = run_direct(d, s);
+    return api_done(e, "grouped_gemm");
 }
 
-hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s) {
-    const bool direct = direct_gemm(g);
-    if (g.R <= few_rows(g, direct) * g.E) return launch_few(g, s);
-    if (direct) return run_direct(g, s);
+int launch_grouped_gemm(const GroupedGemm &g, hipStream_t s) {
+    const bool direct = direct_gemm(g), few = g.R <= few_rows(g, direct) * g.E;
+    if (!few && !direct) {
+        bool done;
+        if (int rc = realigned_gemm(g, s, &done)) return rc;
+        if (done) return EMU_OK;
+    }
     hipError_t e;
-    if (realigned_gemm(g, s, &e)) return e;
-    if (g.dtype == EMU_F32) return launch_staged_gemm_f32(g, s);
-    return g.dtype == EMU_BF16 ? launch_staged_gemm_bf16(g, s) : launch_staged_gemm_f16(g, s);
+    if (few) e = launch_few(g, s);
+    else if (direct) e = run_direct(g, s);
+    else if (g.dtype == EMU_F32) e = launch_staged_gemm_f32(g, s);
+    else e = g.dtype == EMU_BF16 ? launch_staged_gemm_bf16(g, s) : launch_staged_gemm_f16(g, s);
+    return api_done(e, "grouped_gemm");
 }
 
 // Pieces of an expert's rows where the matrices have too few tiles to fill the chip:
@@ -227,7 +235,7 @@ static DirectWgrad direct_wgrad(const GroupedWgrad &g, int tile) {
     return w;
 }
 
-hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
+int launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
     GroupedWgrad d = g;
     const bool f32 = g.dtype == EMU_F32;
     bool direct = !f32 && g.R > 0 && (!g.prow || g.prows > 0) && (!g.qrow || g.qrows > 0);
@@ -245,8 +253,9 @@ hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
     int64_t pb = direct ? w.pb() : 0, qb = direct ? w.qb() : 0;
     const int64_t ld = up(g.N, 4), sums = d.pieces > 1 ? 4 * (int64_t)d.pieces * g.E * g.M * ld : 0;
     char *at = nullptr;
-    if (pb + qb + sums > 0 && api_workspace(pb + qb + sums, &at) != EMU_OK) {
-        api_clear_error();          // no memory: the operands as they are, every expert in one piece
+    if (pb + qb + sums > 0)
+        if (int rc = api_try_workspace(pb + qb + sums, &at)) return rc;
+    if (pb + qb + sums > 0 && !at) {    // the operands as they are, every expert in one piece
         if (direct) w = direct_wgrad(g, 256);
         direct = direct && !w.p && !w.q;
         pb = qb = 0;
@@ -267,7 +276,7 @@ hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
         d.qrows = w.cq.rows;
         if (w.cq.map) d.qrow = nullptr;
     }
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess) return api_done(e, "grouped_wgrad");
     if (d.pieces > 1) {
         d.dW = at + pb + qb;
         d.ldw = ld;
@@ -276,14 +285,14 @@ hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s) {
     if (direct) e = g.dtype == EMU_BF16 ? launch_wgrad16_bf16(d, w.tile, s) : launch_wgrad16_f16(d, w.tile, s);
     else if (f32) e = launch_staged_wgrad_f32(d, s);
     else e = g.dtype == EMU_BF16 ? launch_staged_wgrad_bf16(d, s) : launch_staged_wgrad_f16(d, s);
-    if (e != hipSuccess || d.pieces == 1) return e;
+    if (e != hipSuccess || d.pieces == 1) return api_done(e, "grouped_wgrad");
     with_type(g.dtype, [&](auto z) {
         using T = decltype(z);
         const dim3 grid((unsigned)(((int64_t)g.M * g.N + 255) / 256), g.E);
         join_kernel<T><<<grid, 256, 0, s>>>(reinterpret_cast<const float *>(d.dW), ld, g.M, g.N, d.pieces,
                                             static_cast<T *>(g.dW), g.ldw, g.sw);
     });
-    return hipGetLastError();
+    return api_done(hipGetLastError(), "grouped_wgrad");
 }
 
 }  // namespace emu

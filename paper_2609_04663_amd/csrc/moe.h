@@ -1,5 +1,6 @@
 // Launch wrappers of the mixture-of-experts kernels (arguments checked by the
-// entry points in moe_api.hip).
+// entry points in moe_api.hip).  Those that may ask for workspace return an EMU_*
+// code and set its message, the others HIP's.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -35,7 +36,7 @@ struct GroupedGemm {
     const int *offsets, *rows;
     bool transb;
 };
-hipError_t launch_grouped_gemm(const GroupedGemm &g, hipStream_t s);
+int launch_grouped_gemm(const GroupedGemm &g, hipStream_t s);
 struct GroupedWgrad {
     int dtype, E, M, N;             // dW[e] is M x N = sum over its rows of P[r]^T Q[r]
     int64_t R, prows, qrows;
@@ -47,7 +48,7 @@ struct GroupedWgrad {
     // dW[e pieces + i], ldw a multiple of 4, sw entries apart.
     int pieces;
 };
-hipError_t launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s);
+int launch_grouped_wgrad(const GroupedWgrad &g, hipStream_t s);
 
 // The kernels of 16-bit operands copied straight to LDS (grouped16.h), with square
 // output tiles of 128 or 256; one source file each: they take long to compile.
@@ -77,10 +78,10 @@ struct Q4Gemm {
     int64_t ldx, ldy;
     const int *offsets, *rows;
 };
-hipError_t launch_q4_gemm(const Q4Gemm &g, hipStream_t s);
-hipError_t launch_q4_gemm_f32(const Q4Gemm &g, hipStream_t s);
-hipError_t launch_q4_gemm_bf16(const Q4Gemm &g, hipStream_t s);
-hipError_t launch_q4_gemm_f16(const Q4Gemm &g, hipStream_t s);
+int launch_q4_gemm(const Q4Gemm &g, hipStream_t s);
+int launch_q4_gemm_f32(const Q4Gemm &g, hipStream_t s);
+int launch_q4_gemm_bf16(const Q4Gemm &g, hipStream_t s);
+int launch_q4_gemm_f16(const Q4Gemm &g, hipStream_t s);
 hipError_t launch_q4_pack(int dtype, const void *W, int64_t rows, int64_t ldw, int K, int group,
                           uint8_t *Q, void *scales, hipStream_t s);
 

@@ -20,8 +20,6 @@ int check_type(int dtype) {
     return is_dtype(dtype) ? EMU_OK : api_fail(EMU_EINVAL, "dtype must be EMU_F32, EMU_BF16 or EMU_F16");
 }
 
-int done(hipError_t e, const char *what) { return e == hipSuccess ? EMU_OK : api_hip_fail(e, what); }
-
 int check_route(int dtype, int64_t T, int E, int k, int scope, int64_t ld) {
     if (int rc = check_type(dtype)) return rc;
     if (T < 0 || T > MAX_TOKENS) return api_fail(EMU_EINVAL, "T out of range");
@@ -83,8 +81,8 @@ int emu_moe_route(int dtype, int64_t T, int E, int k, int scope, const void *log
     if (need > 0)
         if (int rc = api_workspace(need, &scratch)) return rc;
     // T = 0: one workgroup without tokens writes the offsets
-    return done(launch_route(dtype, logits, ldl, T, E, k, scope == EMU_ROUTE_ALL, ids, weights, offsets,
-                             rows, slots, scratch, api_stream()), "moe_route");
+    return api_done(launch_route(dtype, logits, ldl, T, E, k, scope == EMU_ROUTE_ALL, ids, weights, offsets,
+                                 rows, slots, scratch, api_stream()), "moe_route");
 }
 
 int emu_moe_route_grad(int dtype, int64_t T, int E, int k, int scope, const void *logits, int64_t ldl,
@@ -96,8 +94,8 @@ int emu_moe_route_grad(int dtype, int64_t T, int E, int k, int scope, const void
         return api_fail(EMU_EINVAL, "NULL pointer");
     api_clear_error();
     if (T == 0) return EMU_OK;
-    return done(launch_route_grad(dtype, logits, ldl, T, E, k, scope == EMU_ROUTE_ALL, ids, weights,
-                                  dweights, dlogits, ldd, api_stream()), "moe_route_grad");
+    return api_done(launch_route_grad(dtype, logits, ldl, T, E, k, scope == EMU_ROUTE_ALL, ids, weights,
+                                      dweights, dlogits, ldd, api_stream()), "moe_route_grad");
 }
 
 int emu_moe_combine(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *Z, int64_t ldz,
@@ -107,8 +105,8 @@ int emu_moe_combine(int dtype, int64_t T, int64_t D, int k, int64_t R, const voi
     if (T > 0 && D > 0 && ((R > 0 && !Z) || !slots || !Y)) return api_fail(EMU_EINVAL, "NULL pointer");
     api_clear_error();
     if (T == 0 || D == 0) return EMU_OK;
-    return done(launch_combine(dtype, Z, ldz, R, T, D, k, slots, weights, Y, ldy, api_stream()),
-                "moe_combine");
+    return api_done(launch_combine(dtype, Z, ldz, R, T, D, k, slots, weights, Y, ldy, api_stream()),
+                    "moe_combine");
 }
 
 int emu_moe_combine_grad(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *dY,
@@ -124,8 +122,8 @@ int emu_moe_combine_grad(int dtype, int64_t T, int64_t D, int k, int64_t R, cons
         return api_fail(EMU_EINVAL, "NULL pointer");
     api_clear_error();
     if (T == 0) return EMU_OK;
-    return done(launch_combine_grad(dtype, dY, lddy, Z, ldz, R, T, D, k, slots, weights, rows, dZ, lddz,
-                                    dweights, api_stream()), "moe_combine_grad");
+    return api_done(launch_combine_grad(dtype, dY, lddy, Z, ldz, R, T, D, k, slots, weights, rows, dZ, lddz,
+                                        dweights, api_stream()), "moe_combine_grad");
 }
 
 int emu_grouped_gemm(int dtype, char transb, int E, int64_t R, int64_t N, int64_t K, const void *X,
@@ -146,7 +144,7 @@ int emu_grouped_gemm(int dtype, char transb, int E, int64_t R, int64_t N, int64_
     api_clear_error();
     if (R == 0 || N == 0) return EMU_OK;
     const GroupedGemm g = {dtype, E, (int)N, (int)K, R, XR, X, W, Y, ldx, ldw, stride, ldy, offsets, rows, tb};
-    return done(launch_grouped_gemm(g, api_stream()), "grouped_gemm");
+    return launch_grouped_gemm(g, api_stream());
 }
 
 int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64_t K, const void *X,
@@ -170,7 +168,7 @@ int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64
                                              ldw, stride, offsets, nullptr, rows, 1}
                               : GroupedWgrad{dtype, E, (int)K, (int)N, R, XR, R, X, dY, dW, ldx, lddy,
                                              ldw, stride, offsets, rows, nullptr, 1};
-    return done(launch_grouped_wgrad(g, api_stream()), "grouped_wgrad");
+    return launch_grouped_wgrad(g, api_stream());
 }
 
 int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, const void *X,
@@ -187,7 +185,7 @@ int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, co
     api_clear_error();
     if (R == 0 || N == 0) return EMU_OK;
     const Q4Gemm g = {dtype, E, (int)N, (int)K, group, R, XR, X, Q, scales, mins, Y, ldx, ldy, offsets, rows};
-    return done(launch_q4_gemm(g, api_stream()), "q4_gemm");
+    return launch_q4_gemm(g, api_stream());
 }
 
 int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, int64_t ldw, uint8_t *Q,
@@ -201,7 +199,7 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
     if (K > 0 && rows > (((int64_t)1 << 32) - 256) / (K / 8)) return api_fail(EMU_EINVAL, "matrix too large");
     api_clear_error();
     if (rows == 0 || K == 0) return EMU_OK;
-    return done(launch_q4_pack(dtype, W, rows, ldw, (int)K, group, Q, scales, api_stream()), "q4_pack");
+    return api_done(launch_q4_pack(dtype, W, rows, ldw, (int)K, group, Q, scales, api_stream()), "q4_pack");
 }
 
 }  // extern "C"

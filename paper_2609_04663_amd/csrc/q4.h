@@ -579,29 +579,29 @@ Q4Plan plan_q4(const Q4Gemm &g) {
 }  // namespace
 
 template <typename T>
-hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
-    hipError_t e = hipSuccess;
+int run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
+    int rc = EMU_OK;
     auto run = [&](auto mt, auto nt, auto set, auto group) {
         constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value, U = decltype(set)::value;
         Q4Plan p = plan_q4<T, MT, NT, U>(g);
         if (p.splits > 1) {
             char *w = nullptr;
-            if (api_workspace(sizeof(float) * p.splits * g.R * g.N, &w) != EMU_OK) {
-                api_clear_error();
-                p.splits = 1;       // no memory: one workgroup for the whole reduction
-            }
+            rc = api_try_workspace(sizeof(float) * p.splits * g.R * g.N, &w);
+            if (rc != EMU_OK) return;
+            if (!w) p.splits = 1;       // one workgroup for the whole reduction
             p.part = reinterpret_cast<float *>(w);
         }
         p.copies = reinterpret_cast<uintptr_t>(g.X) % 16 == 0 && g.ldx % 8 == 0;
         const int cols = 16 * NT * (WAVES / p.wk) * p.passes;
         const int64_t tiles = row_blocks_bound(g.R, g.E, 16 * MT) * ((g.N + cols - 1) / cols);
         q4_gemm_kernel<T, MT, NT, U, decltype(group)::value><<<dim3((unsigned)tiles, p.splits), 64 * WAVES, 0, s>>>(g, p);
-        e = hipGetLastError();
+        hipError_t e = hipGetLastError();
         if (e == hipSuccess && p.splits > 1) {
             q4_join_kernel<T><<<(unsigned)((g.R * g.N + 255) / 256), 256, 0, s>>>(p.part, p.splits, g.R, g.N,
                                                                                   static_cast<T *>(g.Y), g.ldy);
             e = hipGetLastError();
         }
+        rc = api_done(e, "q4_gemm");
     };
     auto rows = [&](auto group) {
         using std::integral_constant;
@@ -624,7 +624,7 @@ hipError_t run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
     if (g.group == 32) rows(std::integral_constant<int, 32>{});
     else if (g.group == 64) rows(std::integral_constant<int, 64>{});
     else rows(std::integral_constant<int, 128>{});
-    return e;
+    return rc;
 }
 
 }  // namespace emu

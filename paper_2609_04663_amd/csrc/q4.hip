@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void q4_pack_kernel(const T *__restrict__ W, i
 
 }  // namespace
 
-hipError_t launch_q4_gemm(const Q4Gemm &g, hipStream_t s) {
+int launch_q4_gemm(const Q4Gemm &g, hipStream_t s) {
     if (g.dtype == EMU_F32) return launch_q4_gemm_f32(g, s);
     if (g.dtype == EMU_BF16) return launch_q4_gemm_bf16(g, s);
     return launch_q4_gemm_f16(g, s);

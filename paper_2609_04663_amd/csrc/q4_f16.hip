@@ -1,7 +1,7 @@
 #include "q4.h"
 
 namespace emu {
-hipError_t launch_q4_gemm_f16(const Q4Gemm &g, hipStream_t s) {
+int launch_q4_gemm_f16(const Q4Gemm &g, hipStream_t s) {
     return run_q4_gemm<half>(g, s);
 }
 }  // namespace emu

@@ -134,6 +134,7 @@ int hipGetSymbolAddress(void **p, const void *var) {
 }
 int hipMalloc(void **p, size_t bytes) {
     *p = nullptr;
+    log("ask", nullptr, (void *)bytes);
     if (int r = unless_captured("hipMalloc")) return r;
     if (held + bytes > room) return result("", OUT_OF_MEMORY);
     *p = calloc(1, bytes < 65536 ? bytes : 65536);      // (kernels do not run)
