@@ -320,8 +320,9 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
    of each have to be on one stream).  A graph and what is outside of it are
    not: the caller orders the graph's launches, and calls outside follow the last
    ones outside.  A captured call must find the workspace grown already (by the
-   same call before the capture; else EMU_ENOMEM, or it does without), and its
-   graph is good until the workspace grows again or is released.  EMU_OK, or EMU_EHIP (the stream remains what it was) if
+   same call before the capture; else EMU_ENOMEM, or it does without).  Its graph
+   is good until emu_release_workspace: a workspace that captured calls use is kept
+   until then when a larger one takes its place.  EMU_OK, or EMU_EHIP (the stream remains what it was) if
    a HIP call fails, or if the new stream is not under capture and would have to
    follow earlier work on one that now is. */
 int emu_set_stream(void *hip_stream);
@@ -346,11 +347,12 @@ int emu_domain_status(unsigned *flags);
    library, valid until the next call. */
 const char *emu_last_error(void);
 
-/* Frees the workspace (synchronises the device first).  The next call
-   allocates again. */
+/* Frees the workspace and those kept for graphs (synchronises the device
+   first).  The next call allocates again. */
 int emu_release_workspace(void);
 
-/* Bytes currently held by the workspace (0 after emu_release_workspace). */
+/* Bytes currently held by the workspace (0 after emu_release_workspace), without
+   those kept for graphs. */
 int64_t emu_workspace_bytes(void);
 
 /* Test hook: the FP32 split of Eq. (fp32split) as the GEMM consumes it.

@@ -68,6 +68,8 @@ struct Workspace {
     size_t refused = (size_t)-1;   // smallest size that the device could not give,
     size_t refused_beside = (size_t)-1;    // and the same beside what is held now
     unsigned status = 0;           // the status word while nothing is held after a refusal
+    bool in_graph = false;         // a captured call uses it: its graph may run at any time
+    std::vector<char *> kept;      // former ones that graphs use, until all is released
 } g_ws;
 
 constexpr size_t HDR = 2048;
@@ -163,9 +165,12 @@ int held_status(unsigned *status) {
 
 int free_held() {
     if (!g_ws.base) return EMU_OK;
-    const hipError_t e = hipFree(g_ws.base);
+    hipError_t e = hipSuccess;
+    if (g_ws.in_graph) g_ws.kept.push_back(g_ws.base);
+    else e = hipFree(g_ws.base);
     g_ws.base = nullptr;
     g_ws.bytes = 0;
+    g_ws.in_graph = false;
     g_ws.refused_beside = (size_t)-1;
     return e == hipSuccess ? EMU_OK : hip_fail(e, "hipFree");
 }
@@ -189,7 +194,10 @@ int ensure_workspace(size_t need) {
     bool capturing = false;
     if (int rc = workspace_user(&capturing)) return rc;
     need += HDR;
-    if (need <= g_ws.bytes) return EMU_OK;
+    if (need <= g_ws.bytes) {
+        g_ws.in_graph |= capturing;
+        return EMU_OK;
+    }
     if (capturing) return fail(EMU_ENOMEM, "the workspace cannot grow while the stream is under capture");
     if (need > workspace_limit()) return fail(EMU_ENOMEM, "workspace would exceed EMU_WORKSPACE_LIMIT");
     unsigned status = 0;
@@ -222,6 +230,7 @@ int try_workspace(size_t need, bool *there) {
     need += HDR;
     if (need <= g_ws.bytes) {
         *there = true;
+        g_ws.in_graph |= capturing;
         return EMU_OK;
     }
     if (capturing || need > workspace_limit() || need >= g_ws.refused || need >= g_ws.refused_beside) return EMU_OK;
@@ -447,10 +456,17 @@ int64_t emu_workspace_bytes(void) { return (int64_t)g_ws.bytes; }
 int emu_release_workspace(void) {
     g_ws.refused = g_ws.refused_beside = (size_t)-1;
     g_ws.status = 0;
-    if (!g_ws.base) return EMU_OK;
-    const hipError_t e = hipDeviceSynchronize();
+    if (!g_ws.base && g_ws.kept.empty()) return EMU_OK;
+    hipError_t e = hipDeviceSynchronize();
     if (e != hipSuccess) return hip_fail(e, "hipDeviceSynchronize");
-    return free_held();
+    g_ws.in_graph = false;
+    int rc = free_held();
+    for (char *p : g_ws.kept) {
+        e = hipFree(p);
+        if (e != hipSuccess) rc = hip_fail(e, "hipFree");
+    }
+    g_ws.kept.clear();
+    return rc;
 }
 
 int emu_profile_enable(int on) {
@@ -497,16 +513,17 @@ int emu_profile_read(int64_t cap, double *split_ms, double *gemm_ms, int64_t *ca
 int emu_domain_status(unsigned *flags) {
     if (!flags) return fail(EMU_EINVAL, "flags is NULL");
     *flags = 0;
-    // the status words of the workspace and of the current device's scratch
+    // the status words of the workspace, of former ones that graphs use, and of the
+    // current device's scratch
     int dev = 0;
-    char *words[2] = {g_ws.base, nullptr};
-    if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < MAX_DEVICES)
-        words[1] = g_scratch_ptr[dev];
-    if (!words[0] && !words[1]) return EMU_OK;
+    std::vector<char *> words = g_ws.kept;
+    if (g_ws.base) words.push_back(g_ws.base);
+    if (hipGetDevice(&dev) == hipSuccess && dev >= 0 && dev < MAX_DEVICES && g_scratch_ptr[dev])
+        words.push_back(g_scratch_ptr[dev]);
+    if (words.empty()) return EMU_OK;
     hipError_t e = hipStreamSynchronize(g_stream);
     if (e != hipSuccess) return hip_fail(e, "hipStreamSynchronize");
     for (char *w : words) {
-        if (!w) continue;
         unsigned f = 0;
         e = hipMemcpy(&f, w, sizeof(unsigned), hipMemcpyDeviceToHost);
         if (e != hipSuccess) return hip_fail(e, "hipMemcpy(status)");

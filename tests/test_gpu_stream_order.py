@@ -73,3 +73,31 @@ def test_calls_before_and_after_a_capture(emu):
         torch.cuda.synchronize()
         assert torch.equal(inside, want[1])
     emu.lib().emu_set_stream(None)
+
+
+def test_a_graph_after_the_workspace_has_grown(emu):
+    """Larger calls, and others' allocations, after the capture."""
+    one, two, inputs = _calls(emu, 4)
+    emu.release_workspace()
+    one(), two()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a, b = one(), two()
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for n in (1024, 3000, 5000):
+        A = torch.randn((n, n), generator=gen, device="cuda")
+        emu.sgemm(A, A)
+        for t in inputs:
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+        want = [one().clone(), two().clone()]
+        torch.cuda.synchronize()
+        a.zero_(), b.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a, want[0]) and torch.equal(b, want[1]), n
+    del graph
+    torch.cuda.synchronize()
+    emu.release_workspace()
+    assert emu.workspace_bytes() == 0
+    emu.lib().emu_set_stream(None)
