@@ -86,7 +86,7 @@ __device__ __forceinline__ bool has_unit(int i) {
 
 // The loads of one operand, ROWS tile rows by the k-block, UNITS runs of eight
 // indices to a thread.  Contiguous along the reduction: row(r) gives the stored
-// row of tile row r or -1 (zeros).
+// row of tile row r, or -1 for zeros (row 0, which must exist, is read and not used).
 template <typename T, int ROWS>
 struct ContigLoads {
     static constexpr int BK = Elem<T>::BK, Q = BK / 8, ALL = ROWS * Q / 64, UNITS = (ALL + 7) / 8;
@@ -319,7 +319,8 @@ __global__ __launch_bounds__(THREADS, 2) void staged_gemm_kernel(GroupedGemm g) 
     const RowTile t = RowTiles(g.offsets, g.E, g.R, AROWS, (g.N + BN - 1) / BN).of_workgroup(blockIdx.x);
     if (t.e < 0) return;
     const int rows = (int)(t.end - t.first), n0 = t.col * BN, cols = g.N - n0 < BN ? g.N - n0 : BN;
-    const bool none = t.e == g.E;               // rows of no expert: an empty reduction gives their zeros
+    // rows of no expert, or an X without rows: an empty reduction gives their zeros
+    const bool none = t.e == g.E || g.xrows == 0;
     const T *const X = static_cast<const T *>(g.X);
     const T *const W = static_cast<const T *>(g.W) + (none ? 0 : t.e * g.sw);
     ContigLoads<T, AROWS> a;

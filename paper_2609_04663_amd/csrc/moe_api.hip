@@ -135,7 +135,8 @@ int emu_grouped_gemm(int dtype, char transb, int E, int64_t R, int64_t N, int64_
     if (ldx < at_least_1(K) || ldw < at_least_1(tb ? K : N) || ldy < at_least_1(N))
         return api_fail(EMU_EINVAL, "leading dimension below the row length");
     if (stride < 0) return api_fail(EMU_EINVAL, "stride < 0");
-    if (R > 0 && N > 0 && (!Y || (K > 0 && E > 0 && (!X || !W)))) return api_fail(EMU_EINVAL, "NULL pointer");
+    if (R > 0 && N > 0 && (!Y || (K > 0 && E > 0 && ((XR > 0 && !X) || !W))))
+        return api_fail(EMU_EINVAL, "NULL pointer");
     if (int rc = check_lds({ldx, ldw, ldy})) return rc;
     // workgroups of 512 threads: on tiles of 16 x 64 or more where the rows are few, else of 128 x 128
     const int64_t tiles = R <= FEW_ROWS * E ? row_blocks_bound(R, E, 16) * ((N + 63) / 64)
@@ -156,7 +157,8 @@ int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64
     if (ldx < at_least_1(K) || lddy < at_least_1(N) || ldw < at_least_1(tb ? K : N))
         return api_fail(EMU_EINVAL, "leading dimension below the row length");
     if (stride < 0) return api_fail(EMU_EINVAL, "stride < 0");
-    if (E > 0 && N > 0 && K > 0 && (!dW || (R > 0 && (!X || !dY)))) return api_fail(EMU_EINVAL, "NULL pointer");
+    if (E > 0 && N > 0 && K > 0 && (!dW || (R > 0 && ((XR > 0 && !X) || !dY))))
+        return api_fail(EMU_EINVAL, "NULL pointer");
     if (int rc = check_lds({ldx, lddy, ldw})) return rc;
     if (E > 1 && N > 0 && K > 0 && stride < ((tb ? N : K) - 1) * ldw + (tb ? K : N))
         return api_fail(EMU_EINVAL, "the matrices of dW overlap");
@@ -179,7 +181,7 @@ int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, co
     if (K % group != 0) return api_fail(EMU_EINVAL, "K must be a multiple of the group");
     if (ldx < at_least_1(K) || ldy < at_least_1(N))
         return api_fail(EMU_EINVAL, "leading dimension below the row length");
-    if (R > 0 && N > 0 && (!Y || (K > 0 && E > 0 && (!X || !Q || !scales))))
+    if (R > 0 && N > 0 && (!Y || (K > 0 && E > 0 && ((XR > 0 && !X) || !Q || !scales))))
         return api_fail(EMU_EINVAL, "NULL pointer");
     if (row_blocks_bound(R, E, 16) * ((N + 15) / 16) > MAX_TILES / 2) return api_fail(EMU_EINVAL, "product too large");
     api_clear_error();

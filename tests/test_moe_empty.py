@@ -1,0 +1,39 @@
+"""An X without rows, which may be NULL: every row number is outside of it and stands
+for a row of zeros (what the library launches, on a stand-in for the HIP runtime)."""
+import pytest
+
+import _fake_hip as F
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    return F.build(tmp_path_factory.mktemp("fake_hip"))
+
+
+@pytest.mark.parametrize("x", ["None", "F.X"])
+def test_no_rows_to_read(fake, x):
+    """Few rows and many, of every type; no kernel that reads a row for one outside."""
+    out = F.run(fake, f"""
+import _fake_hip as F
+result = []
+for dtype in range(3):
+    for transb in "NT":
+        for R in (3, 4000):
+            for K in (512, 513):
+                rc = L.grouped(dtype, transb, 2, R, 256, K, rows=True, XR=0, x={x})
+                result.append([rc, L.kernels()])
+                rc = L.wgrad(dtype, transb, 2, R, 256, K, rows=True, XR=0, x={x})
+                result.append([rc, L.kernels()])
+    for R in (3, 40, 4000):
+        rc = L.q4(dtype, 2, R, 256, 512, rows=True, XR=0, x={x})
+        result.append([rc, L.kernels()])
+""")
+    assert all(rc == 0 and kernels for rc, kernels in out), out
+    assert not any(k.startswith(("gemm16", "wgrad16")) for _, ks in out for k in ks)
+
+
+def test_refused_where_there_are_rows(fake):
+    out = F.run(fake, """
+result = [L.grouped(1, "N", 2, 9, 64, 64, rows=True, XR=1, x=None), L.wgrad(1, "N", 2, 9, 64, 64, rows=True, XR=1, x=None),
+          L.q4(1, 2, 9, 64, 64, rows=True, XR=1, x=None), L.grouped(1, "N", 2, 9, 64, 64, XR=0)]""")
+    assert out == [1, 1, 1, 1]
