@@ -366,10 +366,11 @@ def moe_route(logits: torch.Tensor, k: int, scope: str = "chosen") -> Routing:
     T, E = logits.shape
     _same_gpu(("logits", logits))
     dev = logits.device
-    # one allocation for four (1.5 us each)
-    ids, slots, rows, weights = logits.new_empty((4, T, k), dtype=torch.int32).unbind(0)
-    rows, weights = rows.view(-1), weights.view(torch.float32)
-    offsets = logits.new_empty(E + 1, dtype=torch.int32)
+    # tensors of their own: a caller may keep one, or change one in place while autograd
+    # holds another (as parts of one allocation 1 us less)
+    ids = logits.new_empty((T, k), dtype=torch.int32)
+    slots, weights = torch.empty_like(ids), torch.empty_like(ids, dtype=torch.float32)
+    rows, offsets = ids.new_empty(T * k), ids.new_empty(E + 1)
     _launch(lib().emu_moe_route, dev, code, T, E, k, how, logits.data_ptr(), _ld(logits),
             ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), rows.data_ptr(),
             slots.data_ptr())
