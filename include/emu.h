@@ -302,7 +302,10 @@ int emu_grouped_wgrad(int dtype, char transb, int E, int64_t R, int64_t N, int64
    emu_q4_gemm: Y[r] = X[rows[r]] W[e(r)]^T for R rows ordered by expert as for
    emu_grouped_gemm (offsets NULL: E = 1, every row); made for few rows of each
    expert, where the bytes of Q bound it.  The products are formed with the exact
-   integers q on matrix instructions and scaled per group in FP32. */
+   integers 16 + q on matrix instructions and scaled per group in FP32; a sum that
+   is not finite so (those integers leave FP32's range before W does, at entries of
+   X above some 1e35) is formed again by the definition, in FP64.  So an infinite
+   or NaN entry gives what the definition gives, for FP32 too. */
 int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, const void *X,
                 int64_t ldx, int64_t XR, const int32_t *rows, const uint8_t *Q, const void *scales,
                 const void *mins, const int32_t *offsets, void *Y, int64_t ldy);

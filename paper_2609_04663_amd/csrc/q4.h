@@ -168,7 +168,9 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
     const int col0 = t.col * cols * p.passes;
     float *const part = p.part ? p.part + (int64_t)blockIdx.y * g.R * N : nullptr;
     T *const Y = static_cast<T *>(g.Y);
+    float odd = 0.0f;                                 // NaN where a result was not finite
     auto put = [&](int tok, int col, float v) {
+        odd = fmaf(v, 0.0f, odd);
         if (part) part[(t.first + tok) * N + col] = v;
         else Y[(t.first + tok) * g.ldy + col] = (T)v;
     };
@@ -332,6 +334,36 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
         }
     };
 
+    // A result that was not finite, by the definition in FP64: (16 + q) x or what is taken
+    // off again may have left FP32's range where s (q - 8) x does not, and an infinite
+    // x made it NaN.  8192 x 8192: 0.2 to 1 ms for a row with such an entry; where there is
+    // none, nothing measurable.
+    auto mend = [&](int tok, int col) __attribute__((always_inline)) {
+        T *const y = Y + (t.first + tok) * g.ldy + col;
+        float *const p = part ? part + (t.first + tok) * N + col : nullptr;
+        if (p ? isfinite(*p) : isfinite((float)*y)) return;
+        const int64_t w_row = (int64_t)t.e * N + col;
+        const uint8_t *const q = g.Q + w_row * (K / 2);
+        const T *const s = static_cast<const T *>(g.scales) + w_row * groups;
+        const T *const o = g.mins ? static_cast<const T *>(g.mins) + w_row * groups : nullptr;
+        const T *const x = row_of[tok] < 0 ? nullptr : static_cast<const T *>(g.X) + row_of[tok] * g.ldx;
+        double sum = 0.0;
+#pragma unroll 1
+        for (int k = b_lo * BLOCK; k < k_hi; k += 8) {
+            const unsigned fields = (*reinterpret_cast<const vec<unsigned, 1> *>(q + k / 2))[0];
+            const double scale = (float)s[k / G], offset = o ? (float)o[k / G] : 0.0f;
+            vec<T, 8> v = vec<T, 8>{};
+            if (x) v = *reinterpret_cast<const vec<T, 8> *>(x + k);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int field = fields >> (4 * i) & 15;
+                sum += (o ? scale * field + offset : scale * (field - 8)) * (double)(float)v[i];
+            }
+        }
+        if (p) *p = (float)sum;
+        else *y = (T)(float)sum;
+    };
+
     sums_t y[NT][MT] = {};
     int at[MT][4];                  // the lane's units of a block
 #pragma unroll
@@ -480,6 +512,7 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
         }
         // the pass's results: the lanes' own, or the sums of the waves along the reduction, in order
         const int c0 = col0 + pass * cols;
+        odd = 0.0f;
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             if (wk == 1) {
@@ -511,6 +544,17 @@ __device__ __forceinline__ void q4_tile(const Q4Gemm &g, const Q4Plan &p, const 
             }
 #pragma unroll
             for (int a = 0; a < MT; ++a) y[i][a] = sums_t{};
+        }
+        if (__builtin_expect(odd != odd, 0)) {        // the thread's own results again
+            const int all = m * 16 * wn, per = wk == 1 ? MT * REGS : (all + THREADS - 1) / THREADS;
+#pragma unroll 1
+            for (int n = 0; n < NT * per; ++n) {
+                const int i = n / per, j = n % per, u = threadIdx.x + j * THREADS;
+                const int tok = wk == 1 ? 16 * (j / REGS) + REGS * h + j % REGS : u / (16 * wn);
+                const int of = wk == 1 ? my_n : u / 16 % wn, c = wk == 1 ? lane & 15 : u % 16;
+                const int col = c0 + (of * NT + i) * 16 + c;
+                if (tok < m && col < N && (wk == 1 || u < all)) mend(tok, col);
+            }
         }
         ++pass;
     } while (pass < passes);
