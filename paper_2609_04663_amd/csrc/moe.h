@@ -82,6 +82,11 @@ int launch_q4_gemm(const Q4Gemm &g, hipStream_t s);
 int launch_q4_gemm_f32(const Q4Gemm &g, hipStream_t s);
 int launch_q4_gemm_bf16(const Q4Gemm &g, hipStream_t s);
 int launch_q4_gemm_f16(const Q4Gemm &g, hipStream_t s);
+// Rows of a tile: above 48 of an expert on average 64, for float32 32 (see q4.h).
+inline int q4_tile_rows(int dtype, int64_t R, int64_t E) {
+    const int64_t sets = (R + 16 * E - 1) / (16 * E);
+    return sets <= 3 ? (int)(16 * sets) : (dtype == 0 ? 32 : 64);
+}
 hipError_t launch_q4_pack(int dtype, const void *W, int64_t rows, int64_t ldw, int K, int group,
                           uint8_t *Q, void *scales, hipStream_t s);
 

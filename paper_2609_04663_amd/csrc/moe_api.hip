@@ -183,7 +183,10 @@ int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, co
         return api_fail(EMU_EINVAL, "leading dimension below the row length");
     if (R > 0 && N > 0 && (!Y || (K > 0 && E > 0 && ((XR > 0 && !X) || !Q || !scales))))
         return api_fail(EMU_EINVAL, "NULL pointer");
-    if (row_blocks_bound(R, E, 16) * ((N + 15) / 16) > MAX_TILES / 2) return api_fail(EMU_EINVAL, "product too large");
+    // workgroups of 512 threads: where they are many, a column of 128 or more at a time and sixteen
+    // of these one after the other
+    if (R > 0 && row_blocks_bound(R, E, q4_tile_rows(dtype, R, at_least_1(E))) * ((N + 2047) / 2048) > MAX_TILES / 2)
+        return api_fail(EMU_EINVAL, "product too large");
     api_clear_error();
     if (R == 0 || N == 0) return EMU_OK;
     const Q4Gemm g = {dtype, E, (int)N, (int)K, group, R, XR, X, Q, scales, mins, Y, ldx, ldy, offsets, rows};

@@ -660,10 +660,11 @@ int run_q4_gemm(const Q4Gemm &g, hipStream_t s) {
         // 4096 x 8192 take 40 us, a tile of 64, which spills, 95.
         constexpr bool wide = Q4Elem<T>::PLANES == 3;
         const integral_constant<int, wide ? 1 : 2> set;
-        if (g.R <= 16 * (int64_t)g.E) run(one, one, four, group);
-        else if (g.R <= 32 * (int64_t)g.E) run(two, two, set, group);
-        else if (g.R <= 48 * (int64_t)g.E) run(three, two, set, group);
-        else run(integral_constant<int, wide ? 2 : 4>{}, two, one, group);
+        const int tile = q4_tile_rows(g.dtype, g.R, g.E > 0 ? g.E : 1);
+        if (tile == 16) run(one, one, four, group);
+        else if (tile == 32) run(two, two, set, group);
+        else if (tile == 48) run(three, two, set, group);
+        else if constexpr (!wide) run(four, two, one, group);
     };
     if (g.group == 32) rows(std::integral_constant<int, 32>{});
     else if (g.group == 64) rows(std::integral_constant<int, 64>{});
