@@ -19,8 +19,8 @@ result = [L.q4(dtype, E, R, N, 4096) for dtype in range(3)
 
 
 def test_every_launch_fits(fake):
-    """Below 2^32 threads along an axis, or refused; and refused only for outputs or
-    an X that would take half of the memory of a card."""
+    """Below 2^32 threads along an axis, or refused; and refused only where X, Q and
+    Y would take half of the memory of a card."""
     out = F.run(fake, """
 result = []
 for dtype in range(3):
@@ -29,14 +29,14 @@ for dtype in range(3):
             for N in [1 << i for i in range(0, 30, 3)] + [(1 << 30) - 1]:
                 for K in (64, 8192):
                     rc = L.q4(dtype, E, R, N, K)
-                    result.append([dtype, E, R, N, rc, [l[2:6] for l in L.log() if l[0] == "launch"]])
+                    result.append([dtype, E, R, N, K, rc, [l[2:6] for l in L.log() if l[0] == "launch"]])
 """)
     taken = 0
-    for dtype, E, R, N, rc, launches in out:
+    for dtype, E, R, N, K, rc, launches in out:
         assert rc in (0, 1)
         taken += rc == 0
         for x, y, z, threads in launches:
             assert x * threads < 1 << 32 and y * z < 65536, (dtype, E, R, N)
         if rc == 1:
-            assert R * max(N, 64) * (4 if dtype == 0 else 2) >= 1 << 37, (dtype, E, R, N)
+            assert R * (N + K) * (4 if dtype == 0 else 2) + E * N * K // 2 >= 1 << 37, (dtype, E, R, N, K)
     assert taken > 1500
