@@ -272,7 +272,8 @@ int emu_moe_route_grad(int dtype, int64_t T, int E, int k, int scope, const void
 int emu_moe_combine(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *Z, int64_t ldz,
                     const int32_t *slots, const float *weights, void *Y, int64_t ldy);
 /* Its gradients: dZ[slots[t, j]] = weights[t, j] dY[t], zero for the rows with
-   rows[r] < 0; dweights[t, j] = <Z[slots[t, j]], dY[t]>, 0 for a slot outside Z.
+   rows[r] < 0 (without tokens too); dweights[t, j] = <Z[slots[t, j]], dY[t]>, 0
+   for a slot outside Z.
    slots and rows (R entries) as emu_moe_route gives them. */
 int emu_moe_combine_grad(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *dY,
                          int64_t lddy, const void *Z, int64_t ldz, const int32_t *slots,

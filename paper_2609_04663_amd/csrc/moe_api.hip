@@ -116,12 +116,11 @@ int emu_moe_combine_grad(int dtype, int64_t T, int64_t D, int k, int64_t R, cons
     if (int rc = check_combine(dtype, T, D, k, R)) return rc;
     if (lddy < at_least_1(D) || ldz < at_least_1(D) || lddz < at_least_1(D))
         return api_fail(EMU_EINVAL, "leading dimension < max(1, D)");
-    if (T == 0 && R > 0 && D > 0) return api_fail(EMU_EINVAL, "rows without tokens");
-    if (T > 0 && ((D > 0 && (!dY || (R > 0 && (!Z || !dZ)))) || (R > 0 && !rows) || !slots ||
-                  !weights || !dweights))
+    if (T > 0 && ((D > 0 && (!dY || (R > 0 && !Z))) || !slots || !weights || !dweights))
         return api_fail(EMU_EINVAL, "NULL pointer");
+    if (R > 0 && (!rows || (D > 0 && !dZ))) return api_fail(EMU_EINVAL, "NULL pointer");
     api_clear_error();
-    if (T == 0) return EMU_OK;
+    if (T == 0 && (R == 0 || D == 0)) return EMU_OK;
     return api_done(launch_combine_grad(dtype, dY, lddy, Z, ldz, R, T, D, k, slots, weights, rows, dZ, lddz,
                                         dweights, api_stream()), "moe_combine_grad");
 }

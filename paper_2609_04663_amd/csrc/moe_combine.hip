@@ -70,12 +70,12 @@ __global__ __launch_bounds__(256) void combine_kernel(const T *__restrict__ Z, i
 }
 
 // A workgroup takes a token: its dy stays in registers across the choices, four
-// of which are in flight at a time.  It also clears the rows t, t + T, ... of dz
+// of which are in flight at a time.  It also clears the rows t, t + groups, ... of dz
 // that belong to no token.
 template <typename T>
 __global__ __launch_bounds__(256) void combine_grad_kernel(
     const T *__restrict__ dY, int64_t lddy, const T *__restrict__ Z, int64_t ldz, int64_t R,
-    int64_t tokens, int64_t D, int k, const int *__restrict__ slots, const float *__restrict__ weights,
+    int64_t groups, int64_t D, int k, const int *__restrict__ slots, const float *__restrict__ weights,
     const int *__restrict__ rows, T *__restrict__ dZ, int64_t lddz, float *__restrict__ dweights) {
     constexpr int N = 16 / sizeof(T);
     __shared__ float part[ROUTE_CHOICES][4];
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void combine_grad_kernel(
             if (lane == 0) part[j0 + j][wave] = dot[j];
         }
     }
-    for (int64_t r = t; r < R; r += tokens) {
+    for (int64_t r = t; r < R; r += groups) {
         if (rows[r] >= 0) continue;
         const float zero[N] = {};
         for (int64_t d = threadIdx.x * N; d < D; d += 256 * N)
@@ -153,9 +153,11 @@ hipError_t launch_combine_grad(int dtype, const void *dY, int64_t lddy, const vo
                                float *dweights, hipStream_t s) {
     with_type(dtype, [&](auto z) {
         using type = decltype(z);
-        combine_grad_kernel<type><<<(unsigned)T, 256, 0, s>>>(
-            static_cast<const type *>(dY), lddy, static_cast<const type *>(Z), ldz, R, T, D, k, slots,
-            weights, rows, static_cast<type *>(dZ), lddz, dweights);
+        // no tokens: workgroups without choices clear the rows
+        const int64_t groups = T > 0 ? T : (R < 4096 ? R : 4096);
+        combine_grad_kernel<type><<<(unsigned)groups, 256, 0, s>>>(
+            static_cast<const type *>(dY), lddy, static_cast<const type *>(Z), ldz, R, groups, D, T > 0 ? k : 0,
+            slots, weights, rows, static_cast<type *>(dZ), lddz, dweights);
     });
     return hipGetLastError();
 }

@@ -76,3 +76,14 @@ def test_by_the_c_entry_points(emu):
     rc = L.emu_grouped_gemm(0, b"T", 1, R, N, K, guard.data_ptr(), K, 0, rows.data_ptr(), W.data_ptr(), K, N * K,
                             off.data_ptr(), Y.data_ptr(), N)
     assert rc == emu.EMU_OK and (Y == 0).all()
+
+
+@pytest.mark.parametrize("R", [3, 9000])
+@pytest.mark.parametrize("kind", list(M.TYPES))
+def test_gradient_of_the_combination_without_tokens(emu, kind, R):
+    """A buffer of rows that no token uses: their gradient is zero."""
+    dt, D, k = M.TYPES[kind], 70, 2
+    Z = torch.full((R, D), float("nan"), dtype=dt, device="cuda")
+    dZ, dw = emu.moe_combine_grad(Z[:0], Z, torch.empty((0, k), dtype=torch.int32, device="cuda"),
+                                  torch.empty((0, k), device="cuda"), torch.full((R,), -1, dtype=torch.int32, device="cuda"))
+    assert dZ.shape == (R, D) and (dZ == 0).all() and dw.shape == (0, k)
