@@ -514,7 +514,7 @@ def q4_pack(W: torch.Tensor, group: int = 64):
     if not isinstance(W, torch.Tensor) or W.dim() not in (2, 3):
         raise ValueError("W must be a 2-D or 3-D tensor")
     lead, K = W.shape[:-1], W.shape[-1]
-    flat = W.reshape(-1, K)
+    flat = W.reshape(lead.numel(), K)
     code = _float_mat(flat, "W")
     if group not in (32, 64, 128) or K % group:
         raise ValueError("group must be 32, 64 or 128 and divide K")
