@@ -243,18 +243,27 @@ hipError_t launch_few(const GroupedGemm &g, hipStream_t s) {
     const int nt = tiles(4) < device_cu_count() && (g.transb || g.dtype == EMU_F32) ? 1 : 4;
     with_type(g.dtype, [&](auto z) {
         using T = decltype(z);
-        auto run = [&](auto m, auto n) {
+        constexpr bool F32 = std::is_same<T, float>::value;
+        auto run = [&](auto m, auto n, auto tb) {
             constexpr int MT = decltype(m)::value, NT = decltype(n)::value, THREADS = 64 * Elem<T>::WAVES;
-            if (g.transb) few_kernel<T, MT, NT, true><<<(unsigned)tiles(NT), THREADS, 0, s>>>(g);
-            else few_kernel<T, MT, NT, false><<<(unsigned)tiles(NT), THREADS, 0, s>>>(g);
+            few_kernel<T, MT, NT, decltype(tb)::value><<<(unsigned)tiles(NT), THREADS, 0, s>>>(g);
         };
         const integral_constant<int, 1> one;
         const integral_constant<int, 2> two;
         const integral_constant<int, 4> four;
-        if (mt == 1 && nt == 1) run(one, one);
-        else if (mt == 1) run(one, four);
-        else if (nt == 1) run(two, one);
-        else run(two, four);
+        auto columns = [&](auto m, auto tb) {
+            if constexpr (F32 || decltype(tb)::value)
+                if (nt == 1) return run(m, one, tb);
+            run(m, four, tb);
+        };
+        auto layout = [&](auto tb) {
+            // 16 bits 'T' come here with 8 rows of each expert at most
+            if constexpr (F32 || !decltype(tb)::value)
+                if (mt == 2) return columns(two, tb);
+            columns(one, tb);
+        };
+        if (g.transb) layout(std::true_type{});
+        else layout(std::false_type{});
     });
     return hipGetLastError();
 }
