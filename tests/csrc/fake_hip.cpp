@@ -107,11 +107,16 @@ int __hipPopCallConfiguration(Dim *grid, Dim *block, size_t *shared, void **stre
     *stream = config.stream;
     return 0;
 }
-int hipLaunchKernel(const void *stub, Dim grid, Dim block, void **, size_t, void *stream) {
+int hipLaunchKernel(const void *stub, Dim grid, Dim block, void **args, size_t, void *stream) {
     char line[160];
     snprintf(line, sizeof line, "launch %lld %u %u %u %u ", (long long)(uintptr_t)stream, grid.x, grid.y, grid.z,
              block.x);
     text += line + kernels[stub] + "\n";
+    if (kernels[stub].find("q4_gemm_kernel") != std::string::npos) {
+        const int *plan = static_cast<const int *>(args[1]);    // waves along the reduction, passes, splits
+        snprintf(line, sizeof line, "plan %d %d %d\n", plan[0], plan[1], plan[2]);
+        text += line;
+    }
     return result("hipLaunchKernel");
 }
 int hipGetLastError() {
