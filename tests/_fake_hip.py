@@ -45,11 +45,14 @@ class Library:
         self.emu.emu_last_error.restype = ctypes.c_char_p
         self.emu.emu_workspace_bytes.restype = I64
 
-    def log(self):
+    def log(self, plans=False):
         """The lines since the last call, as lists of words and numbers; a launch
-        is ["launch", stream, x, y, z, threads, kernel]."""
+        is ["launch", stream, x, y, z, threads, kernel].  With plans, those of 4-bit
+        products: ["plan", waves along the reduction, passes, splits]."""
         lines = []
         for line in self.fake.fake_log().decode().splitlines():
+            if line.startswith("plan") and not plans:
+                continue
             words = line.split(" ", 6) if line.startswith("launch") else line.split(" ")
             lines.append([int(w) if w.lstrip("-").isdigit() else w for w in words])
         self.fake.fake_clear()

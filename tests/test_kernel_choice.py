@@ -56,7 +56,7 @@ def test_every_kernel_is_launched_by_some_call(fake):
 def _launches(fake, calls):
     """(kernel, workgroups) of the launches of each call, and a plan's numbers."""
     out = F.run(fake, "result = []\n" + "".join(
-        f"assert {c} == 0\nresult.append(L.log())\n" for c in calls))
+        f"assert {c} == 0\nresult.append(L.log(plans=True))\n" for c in calls))
     return [([(F.short(l[6]), l[2]) for l in log if l[0] == "launch"], [l[1:] for l in log if l[0] == "plan"])
             for log in out]
 
