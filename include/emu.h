@@ -219,7 +219,7 @@ int emu_set_sgemm_split(int mode);
    weights, their gradients and every sum are FP32, rounded once to the output's
    type.  FP32 products are those of emu_sgemm: three BF16 components of each
    operand, six component products, FP32 accumulation (so FP32 accuracy for
-   finite inputs of at least 2^-103 in magnitude; a non-finite entry makes its
+   2^-103 <= |a| < (2 - 2^-8) 2^127; a larger or non-finite entry makes its
    outputs NaN).  They raise no EMU_STATUS_* bits.
    Matrices are row-major with leading dimensions in elements, at any element's
    alignment; index arrays are int32.  Device pointers, ordered on the current
@@ -234,7 +234,8 @@ int emu_set_sgemm_split(int mode);
    The values are read on the device and clamped to the rows that exist, so a
    router's result is passed on without the host's knowledge.
    rows: where given, row r of the product reads row rows[r] of X; an entry
-   outside X stands for a row of zeros.
+   outside X (which may have no row at all) stands for a row of zeros.  Next to
+   a W that is not finite, such a row of a product may be zeros or NaN.
    EMU_EINVAL (before any HIP call) for a bad type, negative sizes, a leading
    dimension below its row length, a NULL pointer to something that is not
    empty, or sizes beyond the limits given.  At most 2^24 - 1 tokens, 2^31 - 1

@@ -17,12 +17,20 @@
 // bank once.  k-blocks of 32 in four stages read 64-byte rows: 5 to 9 % slower.
 //
 // A wave's 256 accumulators leave one workgroup of 256 x 256 to a CU; its tiles run
-// as one stream of k-blocks, the next tile's copies under the stores of the last.
+// as one stream of k-blocks.  The copies of the next tile's first two k-blocks are in
+// flight while a tile is stored, and the wait for the next ones is for the stores too.
 // Measured in bfloat16: 131072 rows over 64 experts of 1024 x 2048, gathered, 557 to
 // 610 us (0.9 to 1.0 PFLOP/s; a large library product reaches 1.47), of which the
-// partly filled last tiles of the experts are 13 % and the stores, which the next
-// tile's first copies wait for, about 100 us.  Its matrix gradient over 65536 rows:
-// 373 to 400 us (0.7 PFLOP/s), bound by the issue of copies and transposing reads.
+// partly filled last tiles of the experts are 13 %; its matrix gradient over 65536
+// rows 339 to 375 us (0.8 PFLOP/s).  The matrix instructions are busy for 49 and
+// 33 % of the cycles, without an LDS bank conflict.  What a part costs, from copies of
+// the kernels that leave it out (us, the product and the gradient):
+//   as it is                  561   349
+//   no stores                 520   299
+//   no copies to LDS          423   278
+//   no reads of fragments     501   349
+//   matrix instructions only  346   213
+// So the copies bound both, then the stores; the transposing reads cost nothing.
 #pragma once
 
 #include "gemm_common.h"
