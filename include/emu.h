@@ -317,6 +317,52 @@ int emu_q4_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, int group, co
 int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, int64_t ldw, uint8_t *Q,
                 void *scales);
 
+/* The balance loss of a routing, for each of S sequences of tokens (1 <= S <= 65536).
+   starts: S + 1 entries, sequence s has the tokens starts[s] to starts[s + 1] (starts[0]
+   counts as 0; not descending, clamped to the T tokens that exist); the tokens from
+   starts[S] on belong to none.  NULL: S = 1, every token.  logits and ids as
+   emu_moe_route has them (entries of ids outside 0 .. E - 1 are not counted).  With p the
+   softmax of a token's logits over all E experts (experts at +inf share it; -inf and NaN
+   have none) and z the logarithm of its sum, n the tokens that have a logit above
+   -inf, c_e the choices of expert e and C = sum c_e:
+     loss[s] = E sum over e of (c_e / C) (1 / n) sum over tokens of p[t, e],
+     zloss[s] = (1 / n) sum over tokens of z[t]^2,
+     counts[s, e] = c_e,  tokens[s] = n
+   (losses 0 where n or C is 0).  Workspace above 256 tokens. */
+int emu_moe_balance(int dtype, int64_t T, int E, int k, int S, const void *logits, int64_t ldl,
+                    const int32_t *ids, const int32_t *starts, float *loss, float *zloss,
+                    int32_t *counts, int32_t *tokens);
+/* Gradient of the logits (T x E, ldd, fully written; zeros for the tokens of no
+   sequence) from the gradients of the losses (S entries; dzloss NULL: zeros), with the
+   shares f_e = c_e / C taken as constant:
+     p[t, e] (dloss E / n (f_e - sum over j of p[t, j] f_j) + dzloss 2 / n z[t]),
+   0 where p is 0 or n is not positive.  counts (S x E) and tokens as emu_moe_balance
+   gives them; where several processes share a batch, their sums. */
+int emu_moe_balance_grad(int dtype, int64_t T, int E, int S, const void *logits, int64_t ldl,
+                         const int32_t *counts, const int32_t *tokens, const int32_t *starts,
+                         const float *dloss, const float *dzloss, void *dlogits, int64_t ldd);
+
+/* Rows in 8-bit integers.  X: rows x K (ldx) of the call's type.  scales[r] =
+   max |x| / 127 of the row, Q (rows x K, ldq) the integer nearest 127 x / max |x|, ties
+   to even, -127 .. 127.  A row of zeros has scale 0; one with an infinity or a NaN
+   has scale NaN and zeros.  emu_q8_unpack: X = scales[r] Q. */
+int emu_q8_pack(int dtype, int64_t rows, int64_t K, const void *X, int64_t ldx, int8_t *Q, int64_t ldq,
+                float *scales);
+int emu_q8_unpack(int dtype, int64_t rows, int64_t K, const int8_t *Q, int64_t ldq, const float *scales,
+                  void *X, int64_t ldx);
+/* Products of rows in 8-bit integers with matrices in 8-bit integers: for R rows ordered
+   by expert as for emu_grouped_gemm (offsets NULL: E = 1, every row)
+     Y[r, n] = xscales[x] wscales[e, n] sum over k of X[x, k] W[e, n, k],
+   e the row's expert and x its row of X, rows[r] (NULL: r itself).  dtype is Y's type.
+   X: XR x K (ldx), xscales XR; W[e] starts at W + e stride and is N x K (ldw), wscales
+   E x N.  Any integers, -128 too; the sums are exact (K <= 131071).  A row of Y whose
+   row of X does not exist is zeros.  Operands whose rows are not multiples of 16 bytes are
+   copied to the workspace first where there are many rows; without workspace, and for
+   few rows, they are read as they are. */
+int emu_q8_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, const int8_t *X, int64_t ldx,
+                const float *xscales, int64_t XR, const int32_t *rows, const int8_t *W, int64_t ldw,
+                int64_t stride, const float *wscales, const int32_t *offsets, void *Y, int64_t ldy);
+
 /* Stream for subsequent calls (a hipStream_t); NULL selects the default
    stream.  Switching streams orders the new stream after the work already
    queued on the previous one (an event dependency, no host synchronisation),

@@ -26,6 +26,11 @@ Mixture-of-experts operators (float32, bfloat16 or float16; see emu.h):
     grouped_wgrad(X, dY, offsets, transb, rows)  -> gradient of W
     q4_pack(W, group)              -> (Q, scales): W in 4 bits
     q4_gemm(X, Q, scales, mins, offsets, rows)   -> Y[r] = X[rows[r]] W[expert of r]^T
+    moe_balance(logits, ids, starts) -> Balance(loss, zloss, counts, tokens) of each sequence
+    moe_balance_grad(logits, counts, tokens, dloss, dzloss, starts) -> gradient of the logits
+    q8_pack(X)                     -> (Q, scales): rows in 8-bit integers, a scale each
+    q8_unpack(Q, scales, dtype)    -> what they stand for
+    q8_gemm(X, xscales, W, wscales, offsets, rows, dtype) -> Y[r] = X[rows[r]] W[expert of r]^T
 """
 from __future__ import annotations
 
@@ -56,7 +61,8 @@ EXPORTS = ("emu_sgemm", "emu_dgemm", "emu_set_stream", "emu_set_split_mode",
            "emu_profile_read", "emu_set_split_scope", "emu_scale_exponents", "emu_sgemm_ex",
            "emu_dgemm_ex", "emu_dgemm_noalloc", "emu_set_fallback", "emu_set_sgemm_split",
            "emu_moe_route", "emu_moe_route_grad", "emu_moe_combine", "emu_moe_combine_grad",
-           "emu_grouped_gemm", "emu_grouped_wgrad", "emu_q4_gemm", "emu_q4_pack")
+           "emu_grouped_gemm", "emu_grouped_wgrad", "emu_q4_gemm", "emu_q4_pack",
+           "emu_moe_balance", "emu_moe_balance_grad", "emu_q8_pack", "emu_q8_unpack", "emu_q8_gemm")
 ROUTE_SCOPES = {"chosen": 0, "all": 1}      # EMU_ROUTE_CHOSEN, EMU_ROUTE_ALL
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # EMU_F32, EMU_BF16, EMU_F16
 
@@ -108,9 +114,15 @@ def lib() -> ctypes.CDLL:
                                         i64]
         L.emu_q4_gemm.argtypes = [ci, ci, i64, i64, i64, ci, p, i64, i64, p, p, p, p, p, p, i64]
         L.emu_q4_pack.argtypes = [ci, i64, i64, ci, p, i64, p, p]
+        L.emu_moe_balance.argtypes = [ci, i64, ci, ci, ci, p, i64, p, p, p, p, p, p]
+        L.emu_moe_balance_grad.argtypes = [ci, i64, ci, ci, p, i64, p, p, p, p, p, p, i64]
+        L.emu_q8_pack.argtypes = [ci, i64, i64, p, i64, p, i64, p]
+        L.emu_q8_unpack.argtypes = [ci, i64, i64, p, i64, p, p, i64]
+        L.emu_q8_gemm.argtypes = [ci, ci, i64, i64, i64, p, i64, p, i64, p, p, i64, i64, p, p, p, i64]
         for name in ("emu_moe_route", "emu_moe_route_grad", "emu_moe_combine",
                      "emu_moe_combine_grad", "emu_grouped_gemm", "emu_grouped_wgrad",
-                     "emu_q4_gemm", "emu_q4_pack"):
+                     "emu_q4_gemm", "emu_q4_pack", "emu_moe_balance", "emu_moe_balance_grad",
+                     "emu_q8_pack", "emu_q8_unpack", "emu_q8_gemm"):
             getattr(L, name).restype = ci
         for name in ("emu_sgemm", "emu_dgemm", "emu_set_stream", "emu_set_split_mode",
                      "emu_domain_status", "emu_release_workspace", "emu_split_f32",
@@ -553,6 +565,136 @@ def q4_gemm(X, Q, scales, mins=None, offsets=None, rows=None, Y=None) -> torch.T
               ("rows", rows), ("Y", Y))
     _launch(lib().emu_q4_gemm, X.device, code, E, R, N, K, group or 32, X.data_ptr(), _ld(X),
             X.shape[0], _ptr(rows), Q.data_ptr(), scales.data_ptr(), _ptr(mins), _ptr(offsets),
+            Y.data_ptr(), _ld(Y))
+    return Y
+
+
+class Balance(NamedTuple):
+    """moe_balance's result for S sequences and E experts (see emu_moe_balance)."""
+    loss: torch.Tensor       # S, float32: E sum_e f_e P_e
+    zloss: torch.Tensor      # S, float32: the mean squared log of the softmax's sum
+    counts: torch.Tensor     # S x E, int32, the choices of each expert
+    tokens: torch.Tensor     # S, int32, the tokens with a logit above -inf
+
+
+def _sequences(starts) -> int:
+    """The number of sequences of the starts (None: one, all tokens)."""
+    if starts is None:
+        return 1
+    if not isinstance(starts, torch.Tensor) or starts.dim() != 1 or starts.shape[0] < 2:
+        raise ValueError("starts must be a 1-D tensor of S + 1 entries")
+    _packed(starts, "starts", torch.int32, starts.shape)
+    return starts.shape[0] - 1
+
+
+def moe_balance(logits, ids, starts=None) -> Balance:
+    """The balance loss, the squared log of the softmax's sum and the experts' counts of
+    a routing; of each sequence, whose tokens are starts[s] to starts[s + 1]."""
+    code, S = _float_mat(logits, "logits"), _sequences(starts)
+    T, E = logits.shape
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids must be a T x k tensor")
+    k = ids.shape[1]
+    _packed(ids, "ids", torch.int32, (T, k))
+    _same_gpu(("logits", logits), ("ids", ids), ("starts", starts))
+    loss = logits.new_empty(S, dtype=torch.float32)
+    zloss, tokens, counts = torch.empty_like(loss), ids.new_empty(S), ids.new_empty((S, E))
+    _launch(lib().emu_moe_balance, logits.device, code, T, E, k, S, logits.data_ptr(), _ld(logits),
+            ids.data_ptr(), _ptr(starts), loss.data_ptr(), zloss.data_ptr(), counts.data_ptr(),
+            tokens.data_ptr())
+    return Balance(loss, zloss, counts, tokens)
+
+
+def moe_balance_grad(logits, counts, tokens, dloss, dzloss=None, starts=None) -> torch.Tensor:
+    """Gradient of the logits from the gradients of moe_balance's losses (dzloss
+    None: zeros); counts and tokens as moe_balance gives them, or sums of several."""
+    code, S = _float_mat(logits, "logits"), _sequences(starts)
+    T, E = logits.shape
+    _packed(counts, "counts", torch.int32, (S, E))
+    _packed(tokens, "tokens", torch.int32, (S,))
+    _packed(dloss, "dloss", torch.float32, (S,))
+    if dzloss is not None:
+        _packed(dzloss, "dzloss", torch.float32, (S,))
+    _same_gpu(("logits", logits), ("counts", counts), ("tokens", tokens), ("dloss", dloss),
+              ("dzloss", dzloss), ("starts", starts))
+    out = logits.new_empty((T, E))
+    _launch(lib().emu_moe_balance_grad, logits.device, code, T, E, S, logits.data_ptr(), _ld(logits),
+            counts.data_ptr(), tokens.data_ptr(), _ptr(starts), dloss.data_ptr(), _ptr(dzloss),
+            out.data_ptr(), E)
+    return out
+
+
+def _int8_mat(t, name: str):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    return _layout(t, torch.int8, name)
+
+
+def _code_of(dtype) -> int:
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+    return code
+
+
+def q8_pack(X: torch.Tensor):
+    """(Q, scales) of the rows of X (two or more dimensions): 8-bit integers of X's
+    shape and a float32 scale for each row (see emu_q8_pack)."""
+    if not isinstance(X, torch.Tensor) or X.dim() < 2:
+        raise ValueError("X must be a tensor of two or more dimensions")
+    lead, K = X.shape[:-1], X.shape[-1]
+    flat = X if X.dim() == 2 else X.reshape(lead.numel(), K)
+    code = _float_mat(flat, "X")
+    _same_gpu(("X", X))
+    Q = torch.empty(X.shape, dtype=torch.int8, device=X.device)
+    scales = torch.empty(lead, dtype=torch.float32, device=X.device)
+    _launch(lib().emu_q8_pack, X.device, code, flat.shape[0], K, flat.data_ptr(), _ld(flat), Q.data_ptr(),
+            max(1, K), scales.data_ptr())
+    return Q, scales
+
+
+def q8_unpack(Q, scales, dtype=torch.bfloat16) -> torch.Tensor:
+    """What q8_pack's integers stand for, scales Q, in this type."""
+    code = _code_of(dtype)
+    if not isinstance(Q, torch.Tensor) or Q.dim() < 2:
+        raise ValueError("Q must be a tensor of two or more dimensions")
+    lead, K = Q.shape[:-1], Q.shape[-1]
+    flat = Q if Q.dim() == 2 else Q.reshape(lead.numel(), K)
+    _int8_mat(flat, "Q")
+    _packed(scales, "scales", torch.float32, lead)
+    _same_gpu(("Q", Q), ("scales", scales))
+    X = torch.empty(Q.shape, dtype=dtype, device=Q.device)
+    _launch(lib().emu_q8_unpack, Q.device, code, flat.shape[0], K, flat.data_ptr(), _ld(flat),
+            scales.data_ptr(), X.data_ptr(), max(1, K))
+    return X
+
+
+def q8_gemm(X, xscales, W, wscales, offsets=None, rows=None, dtype=torch.bfloat16, Y=None) -> torch.Tensor:
+    """Y[r] = X[r] W[e(r)]^T (X[rows[r]] with rows), X and W in 8 bits as q8_pack
+    gives them, Y in `dtype` (with Y given: its own).  W: E x N x K; without
+    offsets one matrix (E = 1, or W N x K) serves every row."""
+    _int8_mat(X, "X")
+    if not isinstance(W, torch.Tensor) or W.dim() not in (2, 3):
+        raise ValueError("W must be a 2-D or 3-D tensor")
+    E, N, K, ldw, stride = _experts(W if W.dim() == 3 else W[None], "W", torch.int8)
+    if X.shape[1] != K:
+        raise ValueError("inner dimensions differ")
+    if offsets is None and E != 1:
+        raise ValueError("more than one matrix needs offsets")
+    _packed(xscales, "xscales", torch.float32, (X.shape[0],))
+    _packed(wscales, "wscales", torch.float32, W.shape[:-1])
+    R = _grouping(X, offsets, rows, E)
+    if Y is None:
+        code = _code_of(dtype)
+        Y = torch.empty((R, N), dtype=dtype, device=X.device)
+    else:
+        code = _float_mat(Y, "Y")
+        if tuple(Y.shape) != (R, N):
+            raise ValueError(f"Y must be {R} x {N}, got {tuple(Y.shape)}")
+    _same_gpu(("X", X), ("xscales", xscales), ("W", W), ("wscales", wscales), ("offsets", offsets),
+              ("rows", rows), ("Y", Y))
+    _launch(lib().emu_q8_gemm, X.device, code, E, R, N, K, X.data_ptr(), _ld(X), xscales.data_ptr(),
+            X.shape[0], _ptr(rows), W.data_ptr(), ldw, stride, wscales.data_ptr(), _ptr(offsets),
             Y.data_ptr(), _ld(Y))
     return Y
 

@@ -1,6 +1,6 @@
 // The grouped products of bfloat16 and half operands whose rows can be copied
 // straight to LDS (16-byte alignment; see direct_gemm and direct_wgrad for the
-// rule).
+// rule).  The stream of k-blocks runs those of 8-bit integers too (q8_tiles.h).
 //
 // A workgroup of 2 x 2 waves computes tiles of 64 RB x 64 RB (256 x 256 or
 // 128 x 128), a wave RB x RB blocks of 32 x 32, by v_mfma 32 x 32 x 16.  A
@@ -53,6 +53,17 @@ __device__ __forceinline__ f32x16 mfma32(frag<bhalf> a, frag<bhalf> b, f32x16 c)
 __device__ __forceinline__ f32x16 mfma32(frag<half> a, frag<half> b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
+// Two 8-bit integers stand for an element of 16 bits: their fragments are 16 bytes of a
+// row too, of 32 indices, and their sums 32-bit integers in the same places.
+using i8pair = int16_t;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+__device__ __forceinline__ i32x16 mfma32(frag<i8pair> a, frag<i8pair> b, i32x16 c) {
+    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0,
+                                                 0);
+}
+template <typename T>
+using sums = std::conditional_t<std::is_same<T, i8pair>::value, i32x16, f32x16>;
 
 // Sixteen zero bytes that copies of rows outside read instead.
 __device__ __attribute__((aligned(16))) float g_zero4[4];
@@ -236,6 +247,7 @@ struct RowSide : StridedSide<RB> {
 //   src.a, src.b     the operands of the tile whose k-blocks are copied next
 //   src.open()       a tile starts (its k-blocks 0 and 1 are copied)
 //   src.trip()       a trip starts
+//   src.arrived(stage, i)   k-block i of the tile whose k-blocks are copied next is in `stage`
 //   src.landed()     no copy is in flight; the next one follows
 //   src.copied()     the copies of a k-block have been started
 //   src.blocks()     k-blocks of the current tile, at least 2
@@ -245,7 +257,7 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
     using A = decltype(src.a);
     using B = decltype(src.b);
     constexpr int STAGE = A::BYTES + B::BYTES, COPIES = A::COPIES + B::COPIES, BLOCKS = RB * RB;
-    f32x16 acc[RB][RB];
+    sums<T> acc[RB][RB];
     auto copy = [&](int c, char *stage) {
         if (c < A::COPIES) src.a.copy(c, src.kb, stage, wave);
         else src.b.copy(c - A::COPIES, src.kb, stage + A::BYTES, wave);
@@ -265,6 +277,7 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
     }
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
     __syncthreads();
+    src.arrived(lds, 0);
     static_for<2 * RB>([&](auto u) { read(f[0], lds, 0, u); });
     int at = 0;                     // the stage of the trip's k-block
     do {
@@ -278,8 +291,8 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
                 Frags &g = f[s & 1], &n = f[1 - (s & 1)];
                 static_for<BLOCKS>([&](auto t_c) {
                     constexpr int t = decltype(t_c)::value;
-                    f32x16 &c = acc[t / RB][t % RB];
-                    c = mfma32(g.b[t % RB], g.a[t / RB], decltype(first)::value && s == 0 ? f32x16{} : c);
+                    sums<T> &c = acc[t / RB][t % RB];
+                    c = mfma32(g.b[t % RB], g.a[t / RB], decltype(first)::value && s == 0 ? sums<T>{} : c);
                     order_fence();
                     static_for<2 * RB>([&](auto u) {
                         if constexpr (u * BLOCKS / (2 * RB) == t) read(n, from, (s + 1) % SUBS, u);
@@ -297,6 +310,7 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
             __builtin_amdgcn_sched_barrier(0);
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             pipeline_barrier();
+            src.arrived(nxt, src.kb - 1);
             src.landed();
             step(std::integral_constant<int, SUBS - 1>{}, nxt, std::true_type{});
             __builtin_amdgcn_sched_barrier(0);
@@ -383,7 +397,8 @@ constexpr int LIST = 64;            // most tiles of a workgroup
 // matrix cores idle, and its control flow costs the accumulators registers).
 struct TileList {
     int4 tile[LIST + 1];            // expert, first row, end, column tile; ends with expert -1
-    __device__ __forceinline__ void fill(const GroupedGemm &g, int rows) {
+    template <typename Gemm>
+    __device__ __forceinline__ void fill(const Gemm &g, int rows) {
         if (threadIdx.x < 64) {
             const RowTiles tiles(g.offsets, g.E, g.R, rows, (g.N + rows - 1) / rows);
             for (int i = 0; i <= LIST; ++i) {
@@ -471,6 +486,7 @@ struct GemmSource {
         look_up();
     }
     __device__ __forceinline__ void trip() {}
+    __device__ __forceinline__ void arrived(char *, int) {}
     __device__ __forceinline__ void landed() {
         if (kb == KB) point();
     }
@@ -585,6 +601,7 @@ struct WgradSource {
             b.preload(kb + 1);
         }
     }
+    __device__ __forceinline__ void arrived(char *, int) {}
     __device__ __forceinline__ void landed() {}
     __device__ __forceinline__ void copied() { ++kb; }
     __device__ __forceinline__ int blocks() const { return blocks_of(now); }

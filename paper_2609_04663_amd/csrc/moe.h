@@ -26,6 +26,28 @@ hipError_t launch_combine_grad(int dtype, const void *dY, int64_t lddy, const vo
                                const float *weights, const int *rows, void *dZ, int64_t lddz,
                                float *dweights, hipStream_t s);
 
+// The balance loss and its gradient; see emu_moe_balance.
+struct BalanceLoss {
+    int dtype, E, k, S;
+    int64_t T, ld;
+    const void *logits;
+    const int *ids, *starts;
+    float *loss, *zloss;
+    int *counts, *tokens;
+};
+struct BalanceGrad {
+    int dtype, E, S;
+    int64_t T, ld, ldd;
+    const void *logits;
+    const int *counts, *tokens, *starts;
+    const float *dloss, *dzloss;
+    void *dlogits;
+};
+// Bytes of scratch that the loss of T tokens in S sequences needs.
+size_t balance_scratch(int64_t T, int E, int S);
+hipError_t launch_balance(const BalanceLoss &b, char *scratch, hipStream_t s);
+hipError_t launch_balance_grad(const BalanceGrad &b, hipStream_t s);
+
 // Products of rows ordered by expert; see emu_grouped_gemm and emu_grouped_wgrad.
 struct GroupedGemm {
     int dtype, E, N, K;
@@ -89,5 +111,28 @@ inline int q4_tile_rows(int dtype, int64_t R, int64_t E) {
 }
 hipError_t launch_q4_pack(int dtype, const void *W, int64_t rows, int64_t ldw, int K, int group,
                           uint8_t *Q, void *scales, hipStream_t s);
+
+// Rows in 8-bit integers and products of such rows; see emu_q8_pack, emu_q8_unpack and emu_q8_gemm.
+hipError_t launch_q8_pack(int dtype, const void *X, int64_t rows, int64_t ldx, int64_t K, int8_t *Q, int64_t ldq,
+                          float *scales, hipStream_t s);
+hipError_t launch_q8_unpack(int dtype, const int8_t *Q, int64_t rows, int64_t ldq, int64_t K, const float *scales,
+                            void *X, int64_t ldx, hipStream_t s);
+struct Q8Gemm {
+    int dtype, E, N, K;             // dtype: of Y
+    int64_t R, xrows;
+    const int8_t *X, *W;
+    const float *xs, *ws;           // a scale for each row of X; for each row of W, E x N
+    void *Y;
+    int64_t ldx, ldw, sw, ldy;
+    const int *offsets, *rows;
+    const int *scaled;              // rows of X that the rows of Y have their scales from: `rows`, also where X is in order
+};
+int launch_q8_gemm(const Q8Gemm &g, hipStream_t s);
+hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s);
+// The kernel of operands copied straight to LDS, with square output tiles of 128 or 256
+// (q8_tiles.h); one source file for each type of Y: they take long to compile.
+hipError_t launch_q8_tiles_f32(const Q8Gemm &g, int tile, hipStream_t s);
+hipError_t launch_q8_tiles_bf16(const Q8Gemm &g, int tile, hipStream_t s);
+hipError_t launch_q8_tiles_f16(const Q8Gemm &g, int tile, hipStream_t s);
 
 }  // namespace emu

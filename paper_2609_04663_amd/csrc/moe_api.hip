@@ -65,6 +65,27 @@ int trans(char t, bool *tr) {
     return EMU_OK;
 }
 
+int check_balance(int dtype, int64_t T, int E, int S, const void *logits, int64_t ldl, const void *starts) {
+    if (int rc = check_type(dtype)) return rc;
+    if (T < 0 || T > MAX_TOKENS) return api_fail(EMU_EINVAL, "T out of range");
+    if (E < 1 || E > ROUTE_EXPERTS) return api_fail(EMU_EINVAL, "E must be 1 to 1024");
+    if (S < 1 || S > 1 << 16) return api_fail(EMU_EINVAL, "S must be 1 to 65536");
+    if (S > 1 && !starts) return api_fail(EMU_EINVAL, "more than one sequence needs starts");
+    if (ldl < E) return api_fail(EMU_EINVAL, "leading dimension < E");
+    if (T > 0 && !logits) return api_fail(EMU_EINVAL, "NULL pointer");
+    return EMU_OK;
+}
+
+// Rows and columns of matrices of 8-bit integers and of what they stand for.
+int check_q8(int dtype, int64_t rows, int64_t K, int64_t ldx, int64_t ldq, const void *X, const void *Q,
+             const void *scales) {
+    if (int rc = check_type(dtype)) return rc;
+    if (rows < 0 || rows > MAX_ROWS || K < 0 || K > MAX_COLS) return api_fail(EMU_EINVAL, "rows or K out of range");
+    if (ldx < at_least_1(K) || ldq < at_least_1(K)) return api_fail(EMU_EINVAL, "leading dimension < max(1, K)");
+    if (rows > 0 && ((K > 0 && (!X || !Q)) || !scales)) return api_fail(EMU_EINVAL, "NULL pointer");
+    return EMU_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -96,6 +117,32 @@ int emu_moe_route_grad(int dtype, int64_t T, int E, int k, int scope, const void
     if (T == 0) return EMU_OK;
     return api_done(launch_route_grad(dtype, logits, ldl, T, E, k, scope == EMU_ROUTE_ALL, ids, weights,
                                       dweights, dlogits, ldd, api_stream()), "moe_route_grad");
+}
+
+int emu_moe_balance(int dtype, int64_t T, int E, int k, int S, const void *logits, int64_t ldl, const int32_t *ids,
+                    const int32_t *starts, float *loss, float *zloss, int32_t *counts, int32_t *tokens) {
+    if (int rc = check_balance(dtype, T, E, S, logits, ldl, starts)) return rc;
+    if (k < 1 || k > E || k > ROUTE_CHOICES) return api_fail(EMU_EINVAL, "k must be 1 to min(E, 32)");
+    if ((T > 0 && !ids) || !loss || !zloss || !counts || !tokens) return api_fail(EMU_EINVAL, "NULL pointer");
+    api_clear_error();
+    char *scratch = nullptr;
+    const size_t need = balance_scratch(T, E, S);
+    if (need > 0)
+        if (int rc = api_workspace(need, &scratch)) return rc;
+    const BalanceLoss b = {dtype, E, k, S, T, ldl, logits, ids, starts, loss, zloss, counts, tokens};
+    return api_done(launch_balance(b, scratch, api_stream()), "moe_balance");
+}
+
+int emu_moe_balance_grad(int dtype, int64_t T, int E, int S, const void *logits, int64_t ldl, const int32_t *counts,
+                         const int32_t *tokens, const int32_t *starts, const float *dloss, const float *dzloss,
+                         void *dlogits, int64_t ldd) {
+    if (int rc = check_balance(dtype, T, E, S, logits, ldl, starts)) return rc;
+    if (ldd < E) return api_fail(EMU_EINVAL, "leading dimension < E");
+    if (T > 0 && (!counts || !tokens || !dloss || !dlogits)) return api_fail(EMU_EINVAL, "NULL pointer");
+    api_clear_error();
+    if (T == 0) return EMU_OK;
+    const BalanceGrad b = {dtype, E, S, T, ldl, ldd, logits, counts, tokens, starts, dloss, dzloss, dlogits};
+    return api_done(launch_balance_grad(b, api_stream()), "moe_balance_grad");
 }
 
 int emu_moe_combine(int dtype, int64_t T, int64_t D, int k, int64_t R, const void *Z, int64_t ldz,
@@ -204,6 +251,43 @@ int emu_q4_pack(int dtype, int64_t rows, int64_t K, int group, const void *W, in
     api_clear_error();
     if (rows == 0 || K == 0) return EMU_OK;
     return api_done(launch_q4_pack(dtype, W, rows, ldw, (int)K, group, Q, scales, api_stream()), "q4_pack");
+}
+
+int emu_q8_pack(int dtype, int64_t rows, int64_t K, const void *X, int64_t ldx, int8_t *Q, int64_t ldq, float *scales) {
+    if (int rc = check_q8(dtype, rows, K, ldx, ldq, X, Q, scales)) return rc;
+    api_clear_error();
+    if (rows == 0) return EMU_OK;
+    return api_done(launch_q8_pack(dtype, X, rows, ldx, K, Q, ldq, scales, api_stream()), "q8_pack");
+}
+
+int emu_q8_unpack(int dtype, int64_t rows, int64_t K, const int8_t *Q, int64_t ldq, const float *scales, void *X,
+                  int64_t ldx) {
+    if (int rc = check_q8(dtype, rows, K, ldx, ldq, X, Q, scales)) return rc;
+    api_clear_error();
+    if (rows == 0 || K == 0) return EMU_OK;
+    return api_done(launch_q8_unpack(dtype, Q, rows, ldq, K, scales, X, ldx, api_stream()), "q8_unpack");
+}
+
+int emu_q8_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, const int8_t *X, int64_t ldx, const float *xscales,
+                int64_t XR, const int32_t *rows, const int8_t *W, int64_t ldw, int64_t stride, const float *wscales,
+                const int32_t *offsets, void *Y, int64_t ldy) {
+    if (int rc = check_grouped(dtype, E, R, N, K, XR, rows, offsets, R > 0 && N > 0 && E != 1)) return rc;
+    if (K > 131071) return api_fail(EMU_EINVAL, "K above 131071: the sums would leave 32 bits");
+    if (ldx < at_least_1(K) || ldw < at_least_1(K) || ldy < at_least_1(N))
+        return api_fail(EMU_EINVAL, "leading dimension below the row length");
+    if (stride < 0) return api_fail(EMU_EINVAL, "stride < 0");
+    if (R > 0 && N > 0 && (!Y || (E > 0 && ((XR > 0 && !xscales) || !wscales || (K > 0 && ((XR > 0 && !X) || !W))))))
+        return api_fail(EMU_EINVAL, "NULL pointer");
+    if (int rc = check_lds({ldx, ldw, ldy})) return rc;
+    // workgroups of 512 threads: on tiles of 16 x 64 or more where the rows are few, else of 128 x 128
+    const int64_t tiles = R <= FEW_ROWS * E ? row_blocks_bound(R, E, 16) * ((N + 63) / 64)
+                                            : row_blocks_bound(R, E, 128) * ((N + 127) / 128);
+    if (tiles > MAX_TILES / 2) return api_fail(EMU_EINVAL, "product too large");
+    api_clear_error();
+    if (R == 0 || N == 0) return EMU_OK;
+    const Q8Gemm g = {dtype, E, (int)N, (int)K, R, XR, X, W, xscales, wscales, Y, ldx, ldw, stride, ldy, offsets,
+                      rows, rows};
+    return launch_q8_gemm(g, api_stream());
 }
 
 }  // extern "C"

@@ -133,6 +133,26 @@ __device__ __forceinline__ T moved(T v) {
     return __builtin_bit_cast(T, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 
+// f over LANES lanes (4, 16 or 64), in all of them; f is associative and commutative but
+// for roundings, which are alike in every lane: f(a, b) and f(b, a) are.
+template <int LANES, typename T, typename F>
+__device__ __forceinline__ T over_lanes(T v, F f) {
+    v = f(v, moved<0xB1>(v));
+    v = f(v, moved<0x4E>(v));
+    if constexpr (LANES > 4) {
+        v = f(v, moved<0x141>(v));
+        v = f(v, moved<0x140>(v));
+    }
+#pragma unroll
+    for (int d = 16; d < LANES; d <<= 1) v = f(v, __shfl_xor(v, d));
+    return v;
+}
+
+// exp(x - m) for x <= m; equal infinities give 1, -inf and NaN 0
+__device__ __forceinline__ float exp_below(float x, float m) {
+    return x == m ? 1.0f : (x > -INFINITY ? expf(x - m) : 0.0f);
+}
+
 // A workgroup's block of rows and its column tile.
 struct RowTile {
     int e;                 // expert; -1: there is no such tile; E: rows of no expert

@@ -45,24 +45,6 @@ __device__ __forceinline__ unsigned ordered(float x) {
 __device__ __forceinline__ float unordered(unsigned o) {
     return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o);
 }
-// exp(x - m) for x <= m; equal infinities give 1, -inf and NaN 0
-__device__ __forceinline__ float exp_below(float x, float m) {
-    return x == m ? 1.0f : (x > -INFINITY ? expf(x - m) : 0.0f);
-}
-
-// f over LANES lanes (16 or 64), in all of them; f is associative and commutative but
-// for roundings, which are alike in every lane: f(a, b) and f(b, a) are.
-template <int LANES, typename T, typename F>
-__device__ __forceinline__ T over_lanes(T v, F f) {
-    v = f(v, moved<0xB1>(v));
-    v = f(v, moved<0x4E>(v));
-    v = f(v, moved<0x141>(v));
-    v = f(v, moved<0x140>(v));
-#pragma unroll
-    for (int d = 16; d < LANES; d <<= 1) v = f(v, __shfl_xor(v, d));
-    return v;
-}
-
 // Bits of a logit in bfloat16 or binary16 as a float that are zero in either.
 constexpr unsigned INDEX = (1u << 13) - 1;
 

@@ -1,0 +1,162 @@
+// The product of 8-bit integers for a few rows of each expert, bound by the bytes of the
+// experts' matrices: every entry of W and X goes from memory to the registers of one wave
+// and from there to the matrix instructions.  Any alignment.
+//
+// v_mfma 16 x 16 x 64 with rows of X as rows and 16 columns of Y as columns.  A wave
+// takes 16 NT columns and 128 indices at a time: a lane loads 16 neighbouring indices of
+// its row or column twice, 64 apart.  The waves of a workgroup take neighbouring runs of
+// 128 and add up their 32-bit sums in LDS at the end; the results are formed in FP64.
+#include "emu_internal.h"
+#include "moe.h"
+#include "moe_common.h"
+
+namespace emu {
+namespace {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int STEP = 128, WAVES = 8, THREADS = 64 * WAVES;
+
+__device__ __forceinline__ i32x4 mfma16(i32x4 a, i32x4 b, i32x4 c) {
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
+}
+
+// Sixteen entries from k on of a row of K, zeros past its end.
+__device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K) {
+    typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
+    if (k + 16 <= K) return *reinterpret_cast<const unaligned *>(row + k);
+    i32x4 v = {};
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        if (k + j < K) v[j / 4] |= (int)(uint8_t)row[k + j] << (8 * (j % 4));
+    return v;
+}
+
+template <int N>
+struct Piece {                      // 128 indices of N rows of a lane
+    i32x4 v[N][2];
+    __device__ __forceinline__ void load(const int8_t *const (&row)[N], int k0, int K, int h) {
+        typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int k = k0 + 64 * p + 16 * h;
+                if (k0 + STEP <= K) v[i][p] = *reinterpret_cast<const unaligned *>(row[i] + k);
+                else v[i][p] = load16(row[i], k, K);
+            }
+    }
+};
+
+// One tile; share: the waves' sums.
+template <typename T, int MT, int NT>
+__device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, int (&share)[WAVES][MT][NT][256]) {
+    constexpr int COLS = 16 * NT;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4;
+    const int m = (int)(t.end - t.first), K = g.K, N = g.N, col0 = t.col * COLS;
+    T *const Y = static_cast<T *>(g.Y) + t.first * g.ldy + col0;
+    if (t.e == g.E) {                                 // rows of no expert
+        for (int i = threadIdx.x; i < m * COLS; i += THREADS)
+            if (col0 + i % COLS < N) Y[i / COLS * g.ldy + i % COLS] = T(0.0f);
+        return;
+    }
+    const int steps = (K + STEP - 1) / STEP, rounds = (steps + WAVES - 1) / WAVES;
+    const int8_t *xrow[MT], *wrow[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        const int n = col0 + 16 * i + (lane & 15);
+        wrow[i] = g.W + t.e * g.sw + (int64_t)(n < N ? n : N - 1) * g.ldw;
+    }
+#pragma unroll
+    for (int a = 0; a < MT; ++a) {                    // rows past the last repeat it, ones outside X row 0
+        const int r = 16 * a + (lane & 15);
+        int64_t at = t.first + (r < m ? r : m - 1);
+        if (g.rows) at = g.rows[at];
+        xrow[a] = g.X + (at >= 0 && at < g.xrows ? at : 0) * g.ldx;
+    }
+    i32x4 acc[MT][NT] = {};
+    Piece<NT> w, w_next;
+    Piece<MT> x, x_next;
+    auto k_of = [&](int round) {
+        const int s = round * WAVES + wave;
+        return (s < steps ? s : steps - 1) * STEP;    // past the end: the last ones, not used
+    };
+    const bool any = rounds > 0 && g.xrows > 0;       // else there is nothing to read
+    if (any) {
+        w_next.load(wrow, k_of(0), K, h);
+        x_next.load(xrow, k_of(0), K, h);
+    }
+    for (int round = 0; any && round < rounds; ++round) {
+        w = w_next;
+        x = x_next;
+        if (round + 1 < rounds) {
+            w_next.load(wrow, k_of(round + 1), K, h);
+            x_next.load(xrow, k_of(round + 1), K, h);
+        }
+        if (round * WAVES + wave < steps) {
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int a = 0; a < MT; ++a) acc[a][i] = mfma16(x.v[a][p], w.v[i][p], acc[a][i]);
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) share[wave][a][i][(4 * h + r) * 16 + (lane & 15)] = acc[a][i][r];
+    __syncthreads();
+    for (int j = threadIdx.x; j < m * COLS; j += THREADS) {
+        const int r = j / COLS, c = j % COLS;
+        if (col0 + c >= N) continue;
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) sum += share[w][r / 16][c / 16][r % 16 * 16 + c % 16];
+        const int64_t at = g.rows ? g.rows[t.first + r] : t.first + r;
+        const bool there = at >= 0 && at < g.xrows;   // zeros for a row outside X, whatever W's scale
+        const double y = there ? (double)sum * g.ws[(int64_t)t.e * N + col0 + c] * g.xs[at] : 0.0;
+        Y[r * g.ldy + c] = (T)(float)y;
+    }
+}
+
+template <typename T, int MT, int NT>
+__global__ __launch_bounds__(THREADS, 2) void q8_few_kernel(Q8Gemm g) {
+    constexpr int COLS = 16 * NT;
+    __shared__ int share[WAVES][MT][NT][256];
+    const RowTiles tiles(g.offsets, g.E, g.R, 16 * MT, (g.N + COLS - 1) / COLS);
+    for (int64_t id = blockIdx.x;; id += gridDim.x) {
+        const RowTile t = tiles.at(id);
+        if (t.e < 0) return;
+        q8_few_tile<T, MT, NT>(g, t, share);
+        __syncthreads();                              // every sum has been read
+    }
+}
+
+}  // namespace
+
+hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s) {
+    using std::integral_constant;
+    const int mt = g.R <= 16 * (int64_t)g.E ? 1 : 2;
+    auto tiles = [&](int nt) { return row_blocks_bound(g.R, g.E, 16 * mt) * ((g.N + 16 * nt - 1) / (16 * nt)); };
+    const int nt = tiles(4) < device_cu_count() ? 1 : 4;
+    with_type(g.dtype, [&](auto z) {
+        using T = decltype(z);
+        auto run = [&](auto m, auto n) {
+            constexpr int MT = decltype(m)::value, NT = decltype(n)::value;
+            constexpr int64_t MOST = 1 << 22;
+            q8_few_kernel<T, MT, NT><<<(unsigned)(tiles(NT) < MOST ? tiles(NT) : MOST), THREADS, 0, s>>>(g);
+        };
+        auto columns = [&](auto m) {
+            if (nt == 1) run(m, integral_constant<int, 1>{});
+            else run(m, integral_constant<int, 4>{});
+        };
+        if (mt == 1) columns(integral_constant<int, 1>{});
+        else columns(integral_constant<int, 2>{});
+    });
+    return hipGetLastError();
+}
+
+}  // namespace emu

@@ -1,0 +1,7 @@
+#include "q8_tiles.h"
+
+namespace emu {
+hipError_t launch_q8_tiles_f32(const Q8Gemm &g, int tile, hipStream_t s) {
+    return launch_q8_tiles<float>(g, tile, s);
+}
+}  // namespace emu
