@@ -238,21 +238,23 @@ struct RowSide : StridedSide<RB> {
 };
 
 // Runs a workgroup's tiles.  Their k-blocks form one stream through two LDS
-// stages: entering a trip the first fragments of its k-block are in registers
+// stages (or STAGES of them: the copies of all but one are in flight): entering a trip the first fragments of its k-block are in registers
 // and the copies of the next k-block are in flight.  Sub-steps 0 to 2 run on the
 // trip's stage; then every wave has read all of it and the next k-block has
 // landed, and during sub-step 3 the copies of the k-block after that start and
 // the first fragments of the next one are read.  At the end of a tile those are
 // the next tile's, so that its results are stored while the copies run.
 //   src.a, src.b     the operands of the tile whose k-blocks are copied next
-//   src.open()       a tile starts (its k-blocks 0 and 1 are copied)
+//   src.open()       a tile starts (its first STAGES k-blocks are copied)
 //   src.trip()       a trip starts
-//   src.arrived(stage, i)   k-block i of the tile whose k-blocks are copied next is in `stage`
+//   src.arrived(stage, i)   a tile's k-block i is in `stage`
 //   src.landed()     no copy is in flight; the next one follows
 //   src.copied()     the copies of a k-block have been started
-//   src.blocks()     k-blocks of the current tile, at least 2
+//   src.blocks()     k-blocks of the current tile, at least STAGES
 //   src.close(acc)   the tile is done; false: it was the last
-template <typename T, int RB, typename Source>
+//   Source::DRAINED  close() waits for every copy before it stores, so that the next tile's
+//                    first trip need not: its stores have two trips to end in
+template <typename T, int RB, int STAGES = 2, typename Source>
 __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
     using A = decltype(src.a);
     using B = decltype(src.b);
@@ -269,13 +271,13 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
         if (u < RB) src.b.template read<T>(g.b, stage + A::BYTES, s, u);
         else src.a.template read<T>(g.a, stage, s, u - RB);
     };
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < STAGES; ++i) {
         src.trip();
         src.landed();
         static_for<COPIES>([&](auto c) { copy(c, lds + i * STAGE); });
         src.copied();
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Source::DRAINED ? 0 : (STAGES - 1) * COPIES) : "memory");
     __syncthreads();
     src.arrived(lds, 0);
     static_for<2 * RB>([&](auto u) { read(f[0], lds, 0, u); });
@@ -283,8 +285,9 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
     do {
         src.open();
         const int KB = src.blocks();
-        auto trip = [&](auto first) {
-            char *const cur = lds + uniform(at), *const nxt = lds + uniform(STAGE - at);
+        auto after = [&](int s) { return STAGES == 2 ? STAGE - s : (s == (STAGES - 1) * STAGE ? 0 : s + STAGE); };
+        auto trip = [&](auto first, int kb) {
+            char *const cur = lds + uniform(at), *const nxt = lds + uniform(after(at));
             // MFMA t, then the reads of the next sub-step whose turn it is, then copies
             auto step = [&](auto s_c, const char *from, auto copies) {
                 constexpr int s = decltype(s_c)::value;
@@ -308,17 +311,22 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
             src.trip();
             static_for<SUBS - 1>([&](auto i) { step(i, cur, std::false_type{}); });
             __builtin_amdgcn_sched_barrier(0);
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            if (Source::DRAINED && decltype(first)::value)
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            else if (STAGES == 2)
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            else
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * COPIES) : "memory");
             pipeline_barrier();
-            src.arrived(nxt, src.kb - 1);
+            src.arrived(nxt, kb + 1 < KB ? kb + 1 : 0);
             src.landed();
             step(std::integral_constant<int, SUBS - 1>{}, nxt, std::true_type{});
             __builtin_amdgcn_sched_barrier(0);
             src.copied();
-            at = STAGE - at;
+            at = after(at);
         };
-        trip(std::true_type{});
-        for (int kb = 1; kb < KB; ++kb) trip(std::false_type{});
+        trip(std::true_type{}, 0);
+        for (int kb = 1; kb < KB; ++kb) trip(std::false_type{}, kb);
     } while (src.close(acc));
     // the last copies are not read: they must land before the workgroup ends
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -418,6 +426,7 @@ struct TileList {
 template <typename T, int RB, bool TB, bool GATHER>
 struct GemmSource {
     static constexpr int TILE = 64 * RB;
+    static constexpr bool DRAINED = false;
     using A = Side<RB, CONTIG>;
     using B = Side<RB, TB ? CONTIG : STRIDED>;
     const GroupedGemm &g;
@@ -526,6 +535,7 @@ __global__ __launch_bounds__(256, RB == 4 ? 1 : 2) void gemm16_kernel(GroupedGem
 template <typename T, int RB, int MAPPED>        // the operand that goes through a map: 0 none, 1 P, 2 Q
 struct WgradSource {
     static constexpr int TILE = 64 * RB;
+    static constexpr bool DRAINED = false;
     static constexpr bool PIECES = RB == 2;     // an expert's rows may be in pieces (the others have no registers to spare)
     using A = RowSide<RB, MAPPED == 1>;
     using B = RowSide<RB, MAPPED == 2>;

@@ -9,8 +9,8 @@
 // a tile).
 //
 // y = x's scale times w's scale times the sum, rounded three times in FP32 (the sum, two
-// products), then to the type.  A column whose scale could take the product with the
-// sum out of FP32's range goes through FP64.
+// products), then to the type.  In a tile where a scale of w could take the product with a
+// sum out of range, mantissas are multiplied and exponents added.
 #pragma once
 
 #include "grouped16.h"
@@ -44,27 +44,41 @@ struct ByteSide : Side<RB, CONTIG> {
     }
 };
 
+// The scales of a tile's rows and columns, which rows exist in X, and whether a column's
+// scale could take its product with a sum out of the range of normal numbers.
+template <int TILE>
+struct Scales {
+    float x[TILE], w[TILE];
+    int there[TILE], wide[TILE / 64];
+};
+
 template <typename T, int RB, bool GATHER>
 struct Q8Source {
     static constexpr int TILE = 64 * RB;
+    static constexpr bool DRAINED = true;
     using A = ByteSide<RB>;
     using B = ByteSide<RB>;
     static_assert(A::COPIES % 2 == 0, "a wave's copies start at an even one");
     const Q8Gemm &g;
     const TileList &list;
+    Scales<TILE> &scales;
     int i;                          // list entry of `next`
     RowTile now, next;              // the tile that is computed, and the one after
     A a;
     B b;
     int kb, KB, chunks, wave, lane;
-    int raw[A::COPIES], row[RB];    // look-ups: of the next tile's copies; X's rows of the rows to store, -1: none
+    int raw[A::COPIES];             // look-ups of the next tile's copies
+    int trips, fetch, row;          // trips of the tile; the one that fetches scales; X's row of its row threadIdx.x
+    float w, x;                     // the scales of the tile's column and row threadIdx.x
 
-    __device__ __forceinline__ Q8Source(const Q8Gemm &g_, const TileList &list_, int wave_, int lane_)
-        : g(g_), list(list_), i(0), wave(wave_), lane(lane_) {
+    __device__ __forceinline__ Q8Source(const Q8Gemm &g_, const TileList &list_, Scales<TILE> &scales_, int wave_,
+                                        int lane_)
+        : g(g_), list(list_), scales(scales_), i(0), wave(wave_), lane(lane_), trips(3) {
         a.init_lane(wave, lane, wave >> 1);
         b.init_lane(wave, lane, wave & 1);
         chunks = g.K / 16;
         KB = chunks <= 2 * KB_CHUNKS ? 2 : (chunks + KB_CHUNKS - 1) / KB_CHUNKS;
+        fetch = KB > 2 ? 1 : 0;         // past the trip in which the last tile's stores end
         now = next = list.at(0);
     }
     // whether the tile is a product (not one of the rows of no expert, the last ones)
@@ -101,11 +115,13 @@ struct Q8Source {
         return true;
     }
     __device__ __forceinline__ void open() {
-#pragma unroll
-        for (int j = 0; j < RB; ++j) {
-            const int64_t r = now.first + ((wave >> 1) * RB + j) * 32 + (lane & 31);
-            row[j] = (int)(r < now.end ? r : now.end - 1);
-            if (g.scaled) row[j] = g.scaled[row[j]];
+        trips = 0;
+        const int tid = threadIdx.x;
+        if (tid < TILE) {
+            const int64_t r = now.first + tid, n = (int64_t)now.col * TILE + tid;
+            row = (int)(r < now.end ? r : now.end - 1);
+            if (g.scaled) row = g.scaled[row];
+            w = g.ws[(int64_t)now.e * g.N + (n < g.N ? n : g.N - 1)];
         }
         // after the last product its own k-blocks are copied again, unused
         const RowTile t = list.at(i + 1);
@@ -114,8 +130,28 @@ struct Q8Source {
         look_up();
     }
     __device__ __forceinline__ void trip() {}
+    // The scales on their way to LDS: in a tile's first trip the row numbers have arrived, in
+    // its second the scales (waiting for them in close() would wait for the copies in
+    // flight, loads return in order, eight times over).
+    __device__ __forceinline__ void fetch_scales() {
+        const int tid = threadIdx.x;
+        if (tid < TILE) {
+            const bool there = row >= 0 && row < g.xrows;
+            if (trips == fetch) x = g.xs[there ? row : 0];
+            if (trips == fetch + 1) {
+                scales.x[tid] = x;
+                scales.w[tid] = w;
+                scales.there[tid] = there;
+                const float m = fabsf(w);
+                const bool wide = __any(m > 0x1p96f || (m < 0x1p-126f && m > 0.0f));
+                if (lane == 0) scales.wide[wave] = wide;
+            }
+        }
+        ++trips;
+    }
     // zeros past the end of X's rows
     __device__ __forceinline__ void arrived(char *stage, int block) {
+        if (trips < fetch + 2) fetch_scales();
         const int first = chunks - block * KB_CHUNKS;
         if (first >= KB_CHUNKS) return;
         const int r = threadIdx.x;
@@ -141,66 +177,71 @@ struct Q8Source {
     // block.  16-bit results are exchanged between the lane halves: eight neighbouring
     // columns of a row to a lane, one 16-byte store.
     __device__ __forceinline__ void store(const i32x16 (&acc)[RB][RB]) const {
-        const int n0 = now.col * TILE, cols = g.N - n0 < TILE ? g.N - n0 : TILE, h = lane >> 5;
-        const float *const ws = g.ws + (int64_t)now.e * g.N + n0;
-        T *const Y = static_cast<T *>(g.Y) + now.first * g.ldy + n0;
-        const int rows = (int)(now.end - now.first);
-        float xs[RB];
-        bool there[RB];                                 // zeros for a row outside X, whatever W's scale
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        pipeline_barrier();                                 // the scales of every wave
+        int wide = 0;
+#pragma unroll
+        for (int i = 0; i < TILE / 64; ++i) wide |= scales.wide[i];
+        wide = uniform(wide);
+        const int rows = (int)(now.end - now.first), cols = g.N - now.col * TILE;
+        if (rows == TILE && cols >= TILE) store_rows<true>(acc, rows, cols, wide);
+        else store_rows<false>(acc, rows, cols, wide);
+    }
+    template <bool FULL>
+    __device__ __forceinline__ void store_rows(const i32x16 (&acc)[RB][RB], int rows, int cols, int wide) const {
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
+        int l = lane;
+        asm volatile("" : "+v"(l));                         // addresses are made here, not kept through the tiles
+        const int h = l >> 5, col0 = (wave & 1) * RB * 32;
+        T *const Y = static_cast<T *>(g.Y) + now.first * g.ldy + now.col * TILE + col0;
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
-            there[i] = row[i] >= 0 && row[i] < g.xrows;
-            xs[i] = g.xs[there[i] ? row[i] : 0];
-        }
+            const int row = ((wave >> 1) * RB + i) * 32 + (l & 31);
+            if (!FULL && row >= rows) continue;
+            T *const p = Y + row * g.ldy + (sizeof(T) == 4 ? 4 : 8) * h;
+            const float x = scales.x[row];
+            const bool keep = scales.there[row];            // zeros for a row outside X, whatever W's scale
 #pragma unroll
-        for (int j = 0; j < RB; ++j)
+            for (int j = 0; j < RB; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; r += 8) {
-                const int col = ((wave & 1) * RB + j) * 32 + 2 * r;     // of 16 columns
-                float w[8];
-                bool wide = false;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int c = col + 8 * (k / 4) + 4 * h + k % 4;
-                    w[k] = ws[c < cols ? c : cols - 1];
-                    const float m = fabsf(w[k]);
-                    wide |= m > 0x1p96f || (m < 0x1p-126f && m > 0.0f);
-                }
-                wide = __any(wide);
-#pragma unroll
-                for (int i = 0; i < RB; ++i) {
+                for (int r = 0; r < 16; r += 8) {
                     __builtin_amdgcn_sched_barrier(0);      // few values in flight: no registers to spare
+                    const int col = j * 32 + 2 * r;         // of 16 columns
+                    const float *const ws = scales.w + col0 + col + 4 * h;
+                    const f32x4 w[2] = {*reinterpret_cast<const f32x4 *>(ws), *reinterpret_cast<const f32x4 *>(ws + 8)};
                     float y[8];
                     if (wide) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) y[k] = (float)((double)acc[i][j][r + k] * w[k] * xs[i]);
+                        for (int k = 0; k < 8; ++k) {
+                            const float m = w[k / 4][k % 4];
+                            y[k] = ldexpf((float)acc[i][j][r + k] * __builtin_amdgcn_frexp_mantf(m) *
+                                              __builtin_amdgcn_frexp_mantf(x),
+                                          __builtin_amdgcn_frexp_expf(m) + __builtin_amdgcn_frexp_expf(x));
+                        }
                     } else {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) y[k] = (float)acc[i][j][r + k] * w[k] * xs[i];
+                        for (int k = 0; k < 8; ++k) y[k] = (float)acc[i][j][r + k] * w[k / 4][k % 4] * x;
                     }
-                    store8(Y, ((wave >> 1) * RB + i) * 32 + (lane & 31), rows, there[i], col, cols, y);
+                    store8<FULL>(p + col, keep, cols - col0 - col, y);
                 }
-            }
+        }
     }
-    // y: columns 4 h .. 4 h + 3 and 8 + 4 h .. of the 16 from col on
-    __device__ __forceinline__ void store8(T *Y, int row, int rows, bool keep, int col, int cols,
-                                           const float (&y)[8]) const {
-        const int h = lane >> 5;
-        T *const p = Y + row * g.ldy;
+    // y: columns 4 h .. 4 h + 3 and 8 + 4 h .. of 16, of which `cols` exist; p: the lane's first
+    template <bool FULL>
+    __device__ __forceinline__ void store8(T *p, bool keep, int cols, float (&y)[8]) const {
         if constexpr (sizeof(T) == 4) {
-            if (row >= rows) return;
+            const int first = 4 * (lane >> 5);
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                const int c = col + 8 * q + 4 * h;
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = keep ? y[4 * q + k] : 0.0f;
-                if (c + 4 <= cols) {
-                    store_f32<4>(p + c, v);
+                if (FULL || first + 8 * q + 4 <= cols) {
+                    store_f32<4>(p + 8 * q, v);
                 } else {
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        if (c + k < cols) p[c + k] = v[k];
+                        if (first + 8 * q + k < cols) p[8 * q + k] = v[k];
                 }
             }
         } else {
@@ -214,16 +255,15 @@ struct Q8Source {
             const u32x2 u = __builtin_amdgcn_permlane32_swap(pack(y[0], y[1]), pack(y[4], y[5]), false, false);
             const u32x2 v = __builtin_amdgcn_permlane32_swap(pack(y[2], y[3]), pack(y[6], y[7]), false, false);
             u32x4 w = {u[0], v[0], u[1], v[1]};
-            if (row >= rows) return;
             if (!keep) w = u32x4{};
-            const int c = col + 8 * h;
             const frag<T> f = __builtin_bit_cast(frag<T>, w);
-            if (c + 8 <= cols) {
-                *reinterpret_cast<vec<T, 8> *>(p + c) = f;
+            const int first = 8 * (lane >> 5);
+            if (FULL || first + 8 <= cols) {
+                *reinterpret_cast<vec<T, 8> *>(p) = f;
             } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (c + k < cols) p[c + k] = f[k];
+                    if (first + k < cols) p[k] = f[k];
             }
         }
     }
@@ -234,9 +274,10 @@ __global__ __launch_bounds__(256, RB == 4 ? 1 : 2) void q8_tiles_kernel(Q8Gemm g
     using Source = Q8Source<T, RB, GATHER>;
     __shared__ __attribute__((aligned(1024))) char lds[2 * (Source::A::BYTES + Source::B::BYTES)];
     __shared__ TileList list;
+    __shared__ __attribute__((aligned(16))) Scales<Source::TILE> scales;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     list.fill(g, Source::TILE);
-    Source src(g, list, wave, lane);
+    Source src(g, list, scales, wave, lane);
     if (src.start()) run_tiles<i8pair, RB>(src, lds, wave);
     // rows of no expert
     for (int i = src.i; list.at(i).e == g.E; ++i) {

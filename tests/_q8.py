@@ -121,5 +121,5 @@ def balance_grad(logits, counts, tokens, dloss, dzloss, starts):
             p, z = got
             mean = (p * f).sum()
             out[t] = p * (dl * (f - mean) + (dz * z if dz else 0.0))
-            bar[t] = 2.0 ** -24 * 200 * p * (abs(dl) * (f + mean) + abs(dz) * (1 + abs(z)))
+            bar[t] = 2.0 ** -24 * 200 * p * (abs(dl) * (f + mean) + (abs(dz) * (1 + abs(z)) if dz else 0.0))
     return out, bar
