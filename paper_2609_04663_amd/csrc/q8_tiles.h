@@ -10,7 +10,9 @@
 //
 // y = x's scale times w's scale times the sum, rounded three times in FP32 (the sum, two
 // products), then to the type.  In a tile where a scale of w could take the product with a
-// sum out of range, mantissas are multiplied and exponents added.
+// sum out of range, mantissas are multiplied and exponents added.  Tiles whose columns all
+// exist, and that need nothing of the kind, are stored without checks: with them the
+// accumulators' way out took half as long again.
 #pragma once
 
 #include "grouped16.h"
@@ -44,12 +46,13 @@ struct ByteSide : Side<RB, CONTIG> {
     }
 };
 
-// The scales of a tile's rows and columns, which rows exist in X, and whether a column's
-// scale could take its product with a sum out of the range of normal numbers.
+// The scales of a tile's rows and columns, which rows exist in X, and (for 64 rows and
+// columns each) whether one does not, or a column's scale could take its product with a
+// sum out of the range of normal numbers.
 template <int TILE>
 struct Scales {
     float x[TILE], w[TILE];
-    int there[TILE], wide[TILE / 64];
+    int there[TILE], special[TILE / 64];
 };
 
 template <typename T, int RB, bool GATHER>
@@ -83,11 +86,18 @@ struct Q8Source {
     }
     // whether the tile is a product (not one of the rows of no expert, the last ones)
     __device__ __forceinline__ bool product(const RowTile &t) const { return t.e >= 0 && t.e < g.E; }
+    // the lane, so that what is made from it is made where it is needed, not kept through the tiles
+    __device__ __forceinline__ int lane_here() const {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    }
     __device__ __forceinline__ void look_up() {
         if constexpr (GATHER) {
+            const int l = lane_here();
 #pragma unroll
             for (int c = 0; c < A::COPIES; ++c) {
-                const int r = (int)next.first + A::row_of(c, wave, lane);
+                const int r = (int)next.first + A::row_of(c, wave, l);
                 raw[c] = g.rows[r < next.end ? r : (int)next.end - 1];
             }
         }
@@ -95,16 +105,16 @@ struct Q8Source {
     // a and b for the tile `next`, from its look-ups; rows outside are read
     // from row 0 and zeroed where they are stored
     __device__ __forceinline__ void point() {
-        const int rows = (int)(next.end - next.first), n0 = next.col * TILE;
+        const int rows = (int)(next.end - next.first), n0 = next.col * TILE, l = lane_here();
         const int cols = g.N - n0 < TILE ? g.N - n0 : TILE;
         const int8_t *const W = g.W + next.e * g.sw + n0 * g.ldw;
         // leading dimensions in pairs
-        a.init(reinterpret_cast<const char *>(g.X + (GATHER ? 0 : next.first * g.ldx)), g.ldx / 2, wave, lane,
+        a.init(reinterpret_cast<const char *>(g.X + (GATHER ? 0 : next.first * g.ldx)), g.ldx / 2, wave, l,
                [&](int c, int r) -> unsigned {
                    if constexpr (!GATHER) return r < rows ? r : rows - 1;
                    return raw[c] >= 0 && raw[c] < g.xrows ? raw[c] : 0;
                });
-        b.init(reinterpret_cast<const char *>(W), g.ldw / 2, wave, lane,
+        b.init(reinterpret_cast<const char *>(W), g.ldw / 2, wave, l,
                [&](int, int r) -> unsigned { return r < cols ? r : cols - 1; });
         kb = 0;
     }
@@ -143,8 +153,8 @@ struct Q8Source {
                 scales.w[tid] = w;
                 scales.there[tid] = there;
                 const float m = fabsf(w);
-                const bool wide = __any(m > 0x1p96f || (m < 0x1p-126f && m > 0.0f));
-                if (lane == 0) scales.wide[wave] = wide;
+                const bool special = __any(!there || m > 0x1p96f || (m < 0x1p-126f && m > 0.0f));
+                if (lane == 0) scales.special[wave] = special;
             }
         }
         ++trips;
@@ -179,55 +189,51 @@ struct Q8Source {
     __device__ __forceinline__ void store(const i32x16 (&acc)[RB][RB]) const {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         pipeline_barrier();                                 // the scales of every wave
-        int wide = 0;
+        int special = 0;
 #pragma unroll
-        for (int i = 0; i < TILE / 64; ++i) wide |= scales.wide[i];
-        wide = uniform(wide);
+        for (int i = 0; i < TILE / 64; ++i) special |= scales.special[i];
         const int rows = (int)(now.end - now.first), cols = g.N - now.col * TILE;
-        if (rows == TILE && cols >= TILE) store_rows<true>(acc, rows, cols, wide);
-        else store_rows<false>(acc, rows, cols, wide);
+        if (cols >= TILE && uniform(special) == 0) store_rows<true>(acc, rows, cols);
+        else store_rows<false>(acc, rows, cols);
     }
-    template <bool FULL>
-    __device__ __forceinline__ void store_rows(const i32x16 (&acc)[RB][RB], int rows, int cols, int wide) const {
+    // PLAIN: every column exists, and nothing is special
+    template <bool PLAIN>
+    __device__ __forceinline__ void store_rows(const i32x16 (&acc)[RB][RB], int rows, int cols) const {
         typedef float f32x4 __attribute__((ext_vector_type(4)));
-        int l = lane;
-        asm volatile("" : "+v"(l));                         // addresses are made here, not kept through the tiles
-        const int h = l >> 5, col0 = (wave & 1) * RB * 32;
+        const int l = lane_here(), h = l >> 5, col0 = (wave & 1) * RB * 32;
         T *const Y = static_cast<T *>(g.Y) + now.first * g.ldy + now.col * TILE + col0;
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
             const int row = ((wave >> 1) * RB + i) * 32 + (l & 31);
-            if (!FULL && row >= rows) continue;
+            if (row >= rows) continue;
             T *const p = Y + row * g.ldy + (sizeof(T) == 4 ? 4 : 8) * h;
             const float x = scales.x[row];
-            const bool keep = scales.there[row];            // zeros for a row outside X, whatever W's scale
+            const bool keep = PLAIN || scales.there[row];   // zeros for a row outside X, whatever W's scale
 #pragma unroll
-            for (int j = 0; j < RB; ++j)
+            for (int j = 0; j < RB; ++j) {
+                __builtin_amdgcn_sched_barrier(0);          // few values in flight: no registers to spare
 #pragma unroll
                 for (int r = 0; r < 16; r += 8) {
-                    __builtin_amdgcn_sched_barrier(0);      // few values in flight: no registers to spare
                     const int col = j * 32 + 2 * r;         // of 16 columns
                     const float *const ws = scales.w + col0 + col + 4 * h;
                     const f32x4 w[2] = {*reinterpret_cast<const f32x4 *>(ws), *reinterpret_cast<const f32x4 *>(ws + 8)};
                     float y[8];
-                    if (wide) {
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const float m = w[k / 4][k % 4];
-                            y[k] = ldexpf((float)acc[i][j][r + k] * __builtin_amdgcn_frexp_mantf(m) *
-                                              __builtin_amdgcn_frexp_mantf(x),
+                    for (int k = 0; k < 8; ++k) {
+                        const float sum = (float)acc[i][j][r + k], m = w[k / 4][k % 4];
+                        if constexpr (PLAIN)
+                            y[k] = sum * m * x;
+                        else
+                            y[k] = ldexpf(sum * __builtin_amdgcn_frexp_mantf(m) * __builtin_amdgcn_frexp_mantf(x),
                                           __builtin_amdgcn_frexp_expf(m) + __builtin_amdgcn_frexp_expf(x));
-                        }
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) y[k] = (float)acc[i][j][r + k] * w[k / 4][k % 4] * x;
                     }
-                    store8<FULL>(p + col, keep, cols - col0 - col, y);
+                    store8<PLAIN>(p + col, keep, cols - col0 - col, y);
                 }
+            }
         }
     }
     // y: columns 4 h .. 4 h + 3 and 8 + 4 h .. of 16, of which `cols` exist; p: the lane's first
-    template <bool FULL>
+    template <bool PLAIN>
     __device__ __forceinline__ void store8(T *p, bool keep, int cols, float (&y)[8]) const {
         if constexpr (sizeof(T) == 4) {
             const int first = 4 * (lane >> 5);
@@ -236,7 +242,7 @@ struct Q8Source {
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = keep ? y[4 * q + k] : 0.0f;
-                if (FULL || first + 8 * q + 4 <= cols) {
+                if (PLAIN || first + 8 * q + 4 <= cols) {
                     store_f32<4>(p + 8 * q, v);
                 } else {
 #pragma unroll
@@ -258,7 +264,7 @@ struct Q8Source {
             if (!keep) w = u32x4{};
             const frag<T> f = __builtin_bit_cast(frag<T>, w);
             const int first = 8 * (lane >> 5);
-            if (FULL || first + 8 <= cols) {
+            if (PLAIN || first + 8 <= cols) {
                 *reinterpret_cast<vec<T, 8> *>(p) = f;
             } else {
 #pragma unroll
