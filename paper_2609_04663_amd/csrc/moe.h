@@ -129,10 +129,12 @@ struct Q8Gemm {
 };
 int launch_q8_gemm(const Q8Gemm &g, hipStream_t s);
 hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s);
-// The kernel of operands copied straight to LDS, with square output tiles of 128 or 256
-// (q8_tiles.h); one source file for each type of Y: they take long to compile.
-hipError_t launch_q8_tiles_f32(const Q8Gemm &g, int tile, hipStream_t s);
-hipError_t launch_q8_tiles_bf16(const Q8Gemm &g, int tile, hipStream_t s);
-hipError_t launch_q8_tiles_f16(const Q8Gemm &g, int tile, hipStream_t s);
+// The kernel of operands copied straight to LDS (q8_tiles.h), with square output tiles of 256,
+// or of 128, two workgroups of two stages on a CU or one of four; one source file for each
+// type of Y: they take long to compile.
+enum class Q8Tiles { LARGE, SMALL, DEEP };
+hipError_t launch_q8_tiles_f32(const Q8Gemm &g, Q8Tiles how, hipStream_t s);
+hipError_t launch_q8_tiles_bf16(const Q8Gemm &g, Q8Tiles how, hipStream_t s);
+hipError_t launch_q8_tiles_f16(const Q8Gemm &g, Q8Tiles how, hipStream_t s);
 
 }  // namespace emu

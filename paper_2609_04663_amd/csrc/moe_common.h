@@ -113,6 +113,11 @@ inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
 
 // A value that all lanes hold, below 2^31, in a scalar register.
 __device__ __forceinline__ int uniform(int64_t v) { return __builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ const char *uniform(const char *p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v), hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
+    return reinterpret_cast<const char *>((uint64_t)hi << 32 | lo);
+}
 
 // v summed over the lanes of the wave up to this one, in register moves between lanes
 // (rows of 16 lanes, then the last lane of one or two rows to those behind).
@@ -242,6 +247,11 @@ __device__ __forceinline__ void copy_lanes(const char *base, unsigned offset, ch
 }
 __device__ __forceinline__ void copy_lanes(const char *src, char *dst) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                 :: "s"(lds_address(dst)), "v"(src) : "memory");
+}
+// The same for 4 bytes of a lane: to dst + 4 l.
+__device__ __forceinline__ void copy_lanes4(const void *src, char *dst) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                  :: "s"(lds_address(dst)), "v"(src) : "memory");
 }
 

@@ -1,5 +1,6 @@
 // Which kernel runs a product of 8-bit integers, and copies of operands whose rows are not
 // multiples of 16 bytes.
+#include <cstdlib>
 #include "api_state.h"
 #include "emu_internal.h"
 #include "moe.h"
@@ -79,9 +80,10 @@ hipError_t run_tiles_kernel(const Q8Gemm &g, hipStream_t s) {
     };
     const int64_t small = tiles(128), rest = small % (2 * cus);
     const double large = (double)((tiles(256) + cus - 1) / cus);
-    const int tile = large <= small / (2 * cus) * 0.58 + (rest > cus ? 0.58 : (rest > 0 ? 0.36 : 0)) ? 256 : 128;
-    if (g.dtype == EMU_F32) return launch_q8_tiles_f32(g, tile, s);
-    return g.dtype == EMU_BF16 ? launch_q8_tiles_bf16(g, tile, s) : launch_q8_tiles_f16(g, tile, s);
+    Q8Tiles how = large <= small / (2 * cus) * 0.58 + (rest > cus ? 0.58 : (rest > 0 ? 0.36 : 0)) ? Q8Tiles::LARGE : Q8Tiles::SMALL;
+    if (const char *e = getenv("Q8HOW")) how = (Q8Tiles)atoi(e);
+    if (g.dtype == EMU_F32) return launch_q8_tiles_f32(g, how, s);
+    return g.dtype == EMU_BF16 ? launch_q8_tiles_bf16(g, how, s) : launch_q8_tiles_f16(g, how, s);
 }
 
 }  // namespace

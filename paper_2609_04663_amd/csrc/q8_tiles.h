@@ -46,16 +46,14 @@ struct ByteSide : Side<RB, CONTIG> {
     }
 };
 
-// The scales of a tile's rows and columns, which rows exist in X, and (for 64 rows and
-// columns each) whether one does not, or a column's scale could take its product with a
-// sum out of the range of normal numbers.
+// The scales of a tile's rows and columns, and which rows exist in X.
 template <int TILE>
 struct Scales {
     float x[TILE], w[TILE];
-    int there[TILE], special[TILE / 64];
+    int there[TILE];
 };
 
-template <typename T, int RB, bool GATHER>
+template <typename T, int RB, int STAGES, bool GATHER>
 struct Q8Source {
     static constexpr int TILE = 64 * RB;
     static constexpr bool DRAINED = true;
@@ -64,24 +62,22 @@ struct Q8Source {
     static_assert(A::COPIES % 2 == 0, "a wave's copies start at an even one");
     const Q8Gemm &g;
     const TileList &list;
-    Scales<TILE> &scales;
+    Scales<TILE> (&scales)[2];      // of the tile and the one after, in turn
     int i;                          // list entry of `next`
     RowTile now, next;              // the tile that is computed, and the one after
     A a;
     B b;
     int kb, KB, chunks, wave, lane;
     int raw[A::COPIES];             // look-ups of the next tile's copies
-    int trips, fetch, row;          // trips of the tile; the one that fetches scales; X's row of its row threadIdx.x
-    float w, x;                     // the scales of the tile's column and row threadIdx.x
+    int row, turn;                  // X's row of row threadIdx.x of the tile that is computed next; 0 or 1
 
-    __device__ __forceinline__ Q8Source(const Q8Gemm &g_, const TileList &list_, Scales<TILE> &scales_, int wave_,
+    __device__ __forceinline__ Q8Source(const Q8Gemm &g_, const TileList &list_, Scales<TILE> (&scales_)[2], int wave_,
                                         int lane_)
-        : g(g_), list(list_), scales(scales_), i(0), wave(wave_), lane(lane_), trips(3) {
+        : g(g_), list(list_), scales(scales_), i(0), wave(wave_), lane(lane_), turn(1) {
         a.init_lane(wave, lane, wave >> 1);
         b.init_lane(wave, lane, wave & 1);
         chunks = g.K / 16;
-        KB = chunks <= 2 * KB_CHUNKS ? 2 : (chunks + KB_CHUNKS - 1) / KB_CHUNKS;
-        fetch = KB > 2 ? 1 : 0;         // past the trip in which the last tile's stores end
+        KB = chunks <= STAGES * KB_CHUNKS ? STAGES : (chunks + KB_CHUNKS - 1) / KB_CHUNKS;
         now = next = list.at(0);
     }
     // whether the tile is a product (not one of the rows of no expert, the last ones)
@@ -93,6 +89,9 @@ struct Q8Source {
         return l;
     }
     __device__ __forceinline__ void look_up() {
+        const int64_t mine = next.first + threadIdx.x;
+        row = (int)(mine < next.end ? mine : next.end - 1);
+        if (g.scaled) row = g.scaled[row];
         if constexpr (GATHER) {
             const int l = lane_here();
 #pragma unroll
@@ -109,12 +108,12 @@ struct Q8Source {
         const int cols = g.N - n0 < TILE ? g.N - n0 : TILE;
         const int8_t *const W = g.W + next.e * g.sw + n0 * g.ldw;
         // leading dimensions in pairs
-        a.init(reinterpret_cast<const char *>(g.X + (GATHER ? 0 : next.first * g.ldx)), g.ldx / 2, wave, l,
+        a.init(uniform(reinterpret_cast<const char *>(g.X + (GATHER ? 0 : next.first * g.ldx))), g.ldx / 2, wave, l,
                [&](int c, int r) -> unsigned {
                    if constexpr (!GATHER) return r < rows ? r : rows - 1;
                    return raw[c] >= 0 && raw[c] < g.xrows ? raw[c] : 0;
                });
-        b.init(reinterpret_cast<const char *>(W), g.ldw / 2, wave, l,
+        b.init(uniform(reinterpret_cast<const char *>(W)), g.ldw / 2, wave, l,
                [&](int, int r) -> unsigned { return r < cols ? r : cols - 1; });
         kb = 0;
     }
@@ -124,14 +123,18 @@ struct Q8Source {
         point();
         return true;
     }
+    // The scales go straight to LDS: waiting for them in registers would wait for the copies
+    // in flight too (loads return in order).  No copy is when a tile starts.
     __device__ __forceinline__ void open() {
-        trips = 0;
-        const int tid = threadIdx.x;
-        if (tid < TILE) {
-            const int64_t r = now.first + tid, n = (int64_t)now.col * TILE + tid;
-            row = (int)(r < now.end ? r : now.end - 1);
-            if (g.scaled) row = g.scaled[row];
-            w = g.ws[(int64_t)now.e * g.N + (n < g.N ? n : g.N - 1)];
+        turn ^= 1;
+        if (wave * 64 < TILE) {
+            Scales<TILE> &s = scales[turn];
+            const int64_t n = (int64_t)now.col * TILE + threadIdx.x;
+            const bool there = row >= 0 && row < g.xrows;
+            s.there[threadIdx.x] = there;
+            copy_lanes4(g.xs + (there ? row : 0), reinterpret_cast<char *>(s.x + wave * 64));
+            copy_lanes4(g.ws + (int64_t)now.e * g.N + (n < g.N ? n : g.N - 1),
+                        reinterpret_cast<char *>(s.w + wave * 64));
         }
         // after the last product its own k-blocks are copied again, unused
         const RowTile t = list.at(i + 1);
@@ -140,28 +143,8 @@ struct Q8Source {
         look_up();
     }
     __device__ __forceinline__ void trip() {}
-    // The scales on their way to LDS: in a tile's first trip the row numbers have arrived, in
-    // its second the scales (waiting for them in close() would wait for the copies in
-    // flight, loads return in order, eight times over).
-    __device__ __forceinline__ void fetch_scales() {
-        const int tid = threadIdx.x;
-        if (tid < TILE) {
-            const bool there = row >= 0 && row < g.xrows;
-            if (trips == fetch) x = g.xs[there ? row : 0];
-            if (trips == fetch + 1) {
-                scales.x[tid] = x;
-                scales.w[tid] = w;
-                scales.there[tid] = there;
-                const float m = fabsf(w);
-                const bool special = __any(!there || m > 0x1p96f || (m < 0x1p-126f && m > 0.0f));
-                if (lane == 0) scales.special[wave] = special;
-            }
-        }
-        ++trips;
-    }
     // zeros past the end of X's rows
     __device__ __forceinline__ void arrived(char *stage, int block) {
-        if (trips < fetch + 2) fetch_scales();
         const int first = chunks - block * KB_CHUNKS;
         if (first >= KB_CHUNKS) return;
         const int r = threadIdx.x;
@@ -189,16 +172,23 @@ struct Q8Source {
     __device__ __forceinline__ void store(const i32x16 (&acc)[RB][RB]) const {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         pipeline_barrier();                                 // the scales of every wave
-        int special = 0;
-#pragma unroll
-        for (int i = 0; i < TILE / 64; ++i) special |= scales.special[i];
+        // whether a row does not exist in X, or a column's scale could take its product with a
+        // sum out of the range of normal numbers
+        const Scales<TILE> &s = scales[turn];
         const int rows = (int)(now.end - now.first), cols = g.N - now.col * TILE;
-        if (cols >= TILE && uniform(special) == 0) store_rows<true>(acc, rows, cols);
-        else store_rows<false>(acc, rows, cols);
+        bool special = cols < TILE;
+#pragma unroll
+        for (int i = lane; i < RB * 32; i += 64) {
+            const float m = fabsf(s.w[(wave & 1) * RB * 32 + i]);
+            special |= !s.there[(wave >> 1) * RB * 32 + i] || m > 0x1p96f || (m < 0x1p-126f && m > 0.0f);
+        }
+        if (__any(special)) store_rows<false>(acc, s, rows, cols);
+        else store_rows<true>(acc, s, rows, cols);
     }
     // PLAIN: every column exists, and nothing is special
     template <bool PLAIN>
-    __device__ __forceinline__ void store_rows(const i32x16 (&acc)[RB][RB], int rows, int cols) const {
+    __device__ __forceinline__ void store_rows(const i32x16 (&acc)[RB][RB], const Scales<TILE> &s, int rows,
+                                               int cols) const {
         typedef float f32x4 __attribute__((ext_vector_type(4)));
         const int l = lane_here(), h = l >> 5, col0 = (wave & 1) * RB * 32;
         T *const Y = static_cast<T *>(g.Y) + now.first * g.ldy + now.col * TILE + col0;
@@ -207,15 +197,15 @@ struct Q8Source {
             const int row = ((wave >> 1) * RB + i) * 32 + (l & 31);
             if (row >= rows) continue;
             T *const p = Y + row * g.ldy + (sizeof(T) == 4 ? 4 : 8) * h;
-            const float x = scales.x[row];
-            const bool keep = PLAIN || scales.there[row];   // zeros for a row outside X, whatever W's scale
+            const float x = s.x[row];
+            const bool keep = PLAIN || s.there[row];   // zeros for a row outside X, whatever W's scale
 #pragma unroll
             for (int j = 0; j < RB; ++j) {
                 __builtin_amdgcn_sched_barrier(0);          // few values in flight: no registers to spare
 #pragma unroll
                 for (int r = 0; r < 16; r += 8) {
                     const int col = j * 32 + 2 * r;         // of 16 columns
-                    const float *const ws = scales.w + col0 + col + 4 * h;
+                    const float *const ws = s.w + col0 + col + 4 * h;
                     const f32x4 w[2] = {*reinterpret_cast<const f32x4 *>(ws), *reinterpret_cast<const f32x4 *>(ws + 8)};
                     float y[8];
 #pragma unroll
@@ -275,16 +265,16 @@ struct Q8Source {
     }
 };
 
-template <typename T, int RB, bool GATHER>
-__global__ __launch_bounds__(256, RB == 4 ? 1 : 2) void q8_tiles_kernel(Q8Gemm g) {
-    using Source = Q8Source<T, RB, GATHER>;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * (Source::A::BYTES + Source::B::BYTES)];
+template <typename T, int RB, int STAGES, bool GATHER>
+__global__ __launch_bounds__(256, RB * STAGES == 4 ? 2 : 1) void q8_tiles_kernel(Q8Gemm g) {
+    using Source = Q8Source<T, RB, STAGES, GATHER>;
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * (Source::A::BYTES + Source::B::BYTES)];
     __shared__ TileList list;
-    __shared__ __attribute__((aligned(16))) Scales<Source::TILE> scales;
+    __shared__ __attribute__((aligned(16))) Scales<Source::TILE> scales[2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     list.fill(g, Source::TILE);
     Source src(g, list, scales, wave, lane);
-    if (src.start()) run_tiles<i8pair, RB>(src, lds, wave);
+    if (src.start()) run_tiles<i8pair, RB, STAGES>(src, lds, wave);
     // rows of no expert
     for (int i = src.i; list.at(i).e == g.E; ++i) {
         const RowTile t = list.at(i);
@@ -297,16 +287,20 @@ __global__ __launch_bounds__(256, RB == 4 ? 1 : 2) void q8_tiles_kernel(Q8Gemm g
 }
 
 template <typename T>
-hipError_t launch_q8_tiles(const Q8Gemm &g, int tile, hipStream_t s) {
-    auto run = [&](auto rb) {
-        constexpr int RB = decltype(rb)::value, TILE = 64 * RB;
+hipError_t launch_q8_tiles(const Q8Gemm &g, Q8Tiles how, hipStream_t s) {
+    auto run = [&](auto rb, auto stages) {
+        constexpr int RB = decltype(rb)::value, STAGES = decltype(stages)::value, TILE = 64 * RB;
         const int64_t tiles = row_blocks_bound(g.R, g.E, TILE) * ((g.N + TILE - 1) / TILE);
-        const unsigned grid = workgroups(tiles, RB == 4 ? 1 : 2);
-        if (g.rows) q8_tiles_kernel<T, RB, true><<<grid, 256, 0, s>>>(g);
-        else q8_tiles_kernel<T, RB, false><<<grid, 256, 0, s>>>(g);
+        const unsigned grid = workgroups(tiles, RB * STAGES == 4 ? 2 : 1);
+        if (g.rows) q8_tiles_kernel<T, RB, STAGES, true><<<grid, 256, 0, s>>>(g);
+        else q8_tiles_kernel<T, RB, STAGES, false><<<grid, 256, 0, s>>>(g);
     };
-    if (tile == 256) run(std::integral_constant<int, 4>{});
-    else run(std::integral_constant<int, 2>{});
+    using std::integral_constant;
+    const integral_constant<int, 2> two;
+    const integral_constant<int, 4> four;
+    if (how == Q8Tiles::LARGE) run(four, two);
+    else if (how == Q8Tiles::SMALL) run(two, two);
+    else run(two, four);
     return hipGetLastError();
 }
 

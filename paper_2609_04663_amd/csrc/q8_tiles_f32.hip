@@ -1,7 +1,7 @@
 #include "q8_tiles.h"
 
 namespace emu {
-hipError_t launch_q8_tiles_f32(const Q8Gemm &g, int tile, hipStream_t s) {
-    return launch_q8_tiles<float>(g, tile, s);
+hipError_t launch_q8_tiles_f32(const Q8Gemm &g, Q8Tiles how, hipStream_t s) {
+    return launch_q8_tiles<float>(g, how, s);
 }
 }  // namespace emu
