@@ -254,7 +254,9 @@ struct RowSide : StridedSide<RB> {
 //   src.close(acc)   the tile is done; false: it was the last
 //   Source::DRAINED  close() waits for every copy before it stores, so that the next tile's
 //                    first trip need not: its stores have two trips to end in
-template <typename T, int RB, int STAGES = 2, typename Source>
+//   LEAD             sub-steps that fragments are read ahead; with 2 the stage is given back a
+//                    sub-step earlier
+template <typename T, int RB, int STAGES = 2, int LEAD = 1, typename Source>
 __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
     using A = decltype(src.a);
     using B = decltype(src.b);
@@ -266,7 +268,8 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
     };
     struct Frags {
         frag<T> a[RB], b[RB];
-    } f[2];
+    } f[2 * LEAD];
+    static_assert(LEAD == 1 || LEAD == 2, "");
     auto read = [&](Frags &g, const char *stage, int s, int u) {
         if (u < RB) src.b.template read<T>(g.b, stage + A::BYTES, s, u);
         else src.a.template read<T>(g.a, stage, s, u - RB);
@@ -277,10 +280,10 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
         static_for<COPIES>([&](auto c) { copy(c, lds + i * STAGE); });
         src.copied();
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(Source::DRAINED ? 0 : (STAGES - 1) * COPIES) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - (Source::DRAINED ? 2 : 1)) * COPIES) : "memory");
     __syncthreads();
     src.arrived(lds, 0);
-    static_for<2 * RB>([&](auto u) { read(f[0], lds, 0, u); });
+    static_for<LEAD>([&](auto s) { static_for<2 * RB>([&](auto u) { read(f[s], lds, s, u); }); });
     int at = 0;                     // the stage of the trip's k-block
     do {
         src.open();
@@ -290,26 +293,26 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
             char *const cur = lds + uniform(at), *const nxt = lds + uniform(after(at));
             // MFMA t, then the reads of the next sub-step whose turn it is, then copies
             auto step = [&](auto s_c, const char *from, auto copies) {
-                constexpr int s = decltype(s_c)::value;
-                Frags &g = f[s & 1], &n = f[1 - (s & 1)];
+                constexpr int s = decltype(s_c)::value, ahead = (s + LEAD) % SUBS;
+                Frags &g = f[s % (2 * LEAD)], &n = f[ahead % (2 * LEAD)];
                 static_for<BLOCKS>([&](auto t_c) {
                     constexpr int t = decltype(t_c)::value;
                     sums<T> &c = acc[t / RB][t % RB];
                     c = mfma32(g.b[t % RB], g.a[t / RB], decltype(first)::value && s == 0 ? sums<T>{} : c);
                     order_fence();
                     static_for<2 * RB>([&](auto u) {
-                        if constexpr (u * BLOCKS / (2 * RB) == t) read(n, from, (s + 1) % SUBS, u);
+                        if constexpr (u * BLOCKS / (2 * RB) == t) read(n, from, ahead, u);
                     });
                     order_fence();
                     if constexpr (decltype(copies)::value)
                         static_for<COPIES>([&](auto i) {
-                            if constexpr (i * BLOCKS / COPIES == t) copy(i, cur);
+                            if constexpr (i * LEAD * BLOCKS / COPIES == (s - SUBS + LEAD) * BLOCKS + t) copy(i, cur);
                         });
                     order_fence();
                 });
             };
             src.trip();
-            static_for<SUBS - 1>([&](auto i) { step(i, cur, std::false_type{}); });
+            static_for<SUBS - LEAD>([&](auto i) { step(i, cur, std::false_type{}); });
             __builtin_amdgcn_sched_barrier(0);
             if (Source::DRAINED && decltype(first)::value)
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -320,7 +323,9 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
             pipeline_barrier();
             src.arrived(nxt, kb + 1 < KB ? kb + 1 : 0);
             src.landed();
-            step(std::integral_constant<int, SUBS - 1>{}, nxt, std::true_type{});
+            static_for<LEAD>([&](auto i) {
+                step(std::integral_constant<int, SUBS - LEAD + decltype(i)::value>{}, nxt, std::true_type{});
+            });
             __builtin_amdgcn_sched_barrier(0);
             src.copied();
             at = after(at);

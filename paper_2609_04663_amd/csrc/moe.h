@@ -129,6 +129,7 @@ struct Q8Gemm {
 };
 int launch_q8_gemm(const Q8Gemm &g, hipStream_t s);
 hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s);
+double q8_few_traffic(const Q8Gemm &g);     // bytes that its waves read, of X and W (E > 0)
 // The kernel of operands copied straight to LDS (q8_tiles.h), with square output tiles of 256,
 // or of 128, two workgroups of two stages on a CU or one of four; one source file for each
 // type of Y: they take long to compile.

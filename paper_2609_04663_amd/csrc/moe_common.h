@@ -110,6 +110,12 @@ __device__ inline int64_t first_tile_of_xcd(const int *__restrict__ offsets, int
 inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
     return R / rows + (E + 1 < R ? E + 1 : R);
 }
+// About so many: an expert's last block is half full on average.
+inline int64_t row_blocks_expected(int64_t R, int64_t E, int64_t rows) {
+    if (E == 1) return (R + rows - 1) / rows;
+    const int64_t blocks = (R + E * rows / 2) / rows, least = R < E ? R : E;
+    return blocks > least ? blocks : least;
+}
 
 // A value that all lanes hold, below 2^31, in a scalar register.
 __device__ __forceinline__ int uniform(int64_t v) { return __builtin_amdgcn_readfirstlane((int)v); }

@@ -1,6 +1,5 @@
 // Which kernel runs a product of 8-bit integers, and copies of operands whose rows are not
 // multiples of 16 bytes.
-#include <cstdlib>
 #include "api_state.h"
 #include "emu_internal.h"
 #include "moe.h"
@@ -29,22 +28,25 @@ struct Copied {
     int64_t bytes() const { return mats * rows * ld; }
 };
 
-// 16 bytes a thread: unaligned loads, aligned stores.  Bound by bytes.
-__global__ __launch_bounds__(256) void q8_copy_kernel(Copied m, int8_t *__restrict__ dst) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int per_row = (int)(m.ld / 16);
+// 16 bytes a thread: unaligned loads, aligned stores; blockIdx.y is X or a matrix of W.
+// Bound by bytes.
+__global__ __launch_bounds__(256) void q8_copy_kernel(Copied x, int8_t *__restrict__ to_x, Copied w,
+                                                      int8_t *__restrict__ to_w) {
+    const bool is_x = blockIdx.y < x.mats;
+    const Copied m = is_x ? x : w;
+    const unsigned i = blockIdx.x * 256 + threadIdx.x, per_row = (unsigned)(m.ld / 16);
     const int64_t row = i / per_row;
     const int c = (int)(i % per_row) * 16;
     if (row >= m.rows) return;
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
-    for (int e = blockIdx.y; e < m.mats; e += gridDim.y) {
+    const int64_t at = m.map ? m.map[row] : row;
+    for (int e = is_x ? 0 : blockIdx.y - x.mats; e < m.mats; e += gridDim.y - x.mats) {
         if (m.offsets) {
             int64_t lo, hi;
             expert_rows(m.offsets, m.mats, m.R, e, lo, hi);
             if (lo == hi) continue;
         }
-        const int64_t at = m.map ? m.map[row] : row;
         i32x4 v = {};
         if (at >= 0 && at < m.src_rows) {
             const int8_t *const p = m.src + e * m.stride + at * m.lds + c;
@@ -56,12 +58,14 @@ __global__ __launch_bounds__(256) void q8_copy_kernel(Copied m, int8_t *__restri
                     if (c + j < m.cols) v[j / 4] |= (int)(uint8_t)p[j] << (8 * (j % 4));
             }
         }
-        *reinterpret_cast<i32x4 *>(dst + (e * m.rows + row) * m.ld + c) = v;
+        *reinterpret_cast<i32x4 *>((is_x ? to_x : to_w) + (e * m.rows + row) * m.ld + c) = v;
+        if (is_x) return;
     }
 }
-hipError_t copy(const Copied &m, char *dst, hipStream_t s) {
-    const dim3 grid((unsigned)((m.rows * m.ld / 16 + 255) / 256), m.mats < 32768 ? m.mats : 32768);
-    q8_copy_kernel<<<grid, 256, 0, s>>>(m, reinterpret_cast<int8_t *>(dst));
+hipError_t copy(const Copied &x, char *to_x, const Copied &w, char *to_w, hipStream_t s) {
+    const int64_t nx = x.mats * x.rows * x.ld, nw = w.mats > 0 ? w.rows * w.ld : 0, n = nx > nw ? nx : nw;
+    const dim3 grid((unsigned)((n / 16 + 255) / 256), x.mats + (w.mats < 32768 ? w.mats : 32768));
+    q8_copy_kernel<<<grid, 256, 0, s>>>(x, reinterpret_cast<int8_t *>(to_x), w, reinterpret_cast<int8_t *>(to_w));
     return hipGetLastError();
 }
 
@@ -72,16 +76,34 @@ bool fits_tiles(const Q8Gemm &g) {
            (!g.rows || g.xrows > 0);
 }
 
+// Times, us, that the choice between the two kernels goes by.  Measured, that for few rows
+// and that of tiles: 16 rows of 8192 x 8192 20 and 30; 64 rows of 4096 x 4096 14 and 18, 128 rows
+// 17 and 19; 100 rows of 8192 x 4096 22 and 18, 300 rows 57 and 21; 64 experts of 2048 x 2048,
+// 8 rows 10 and 16, 32 rows 25 and 19, 128 rows 47 and 38, 4096 rows 144 and 50; 13 of 1501 x 777,
+// 100 rows 15 and 24 (with the copies).
+int64_t tiles_of(const Q8Gemm &g, int64_t t) { return row_blocks_expected(g.R, g.E, t) * ((g.N + t - 1) / t); }
+double matrix_bytes(const Q8Gemm &g) { return (double)(g.R < g.E ? g.R : g.E) * g.N * g.K; }
+// The kernel for few rows: its waves read at 8 TB/s, at half of it from rows that are not
+// multiples of 16 bytes.
+double time_of_few(const Q8Gemm &g) { return 5 + q8_few_traffic(g) / (g.K % 16 == 0 ? 8e6 : 4e6); }
+// Tiles of 128 take 0.45 us for a k-block (copies to LDS at 64 bytes a cycle and the reads of
+// fragments), all of them the matrices' bytes at 6 TB/s.
+double time_of_tiles(const Q8Gemm &g) {
+    const int64_t cus = device_cu_count(), blocks = (g.K + 127) / 128;
+    const double copies = (double)((tiles_of(g, 128) + cus - 1) / cus) * blocks * 0.45, bytes = matrix_bytes(g) / 6e6;
+    return (g.E > 1 ? 7 : 4) + (copies > bytes ? copies : bytes);
+}
+
+// Rounds of one tile of 256 on a CU; of two of 128, 0.58 of that long, or 0.45 where half the
+// places stay empty; of one of 128 in four stages, 0.29, for long reductions (it starts when
+// all four are there).  8192 x 8192 x 8192: 449, 521 and 603 us; 2048 x 4096 x 4096: 52, 40 and
+// 43; 300 rows of 8192 x 4096: 49, 27 and 21; 200 over 8 experts of 2048 x 1024: SMALL 9, DEEP 12.
 hipError_t run_tiles_kernel(const Q8Gemm &g, hipStream_t s) {
-    const int64_t cus = device_cu_count();
-    auto tiles = [&](int64_t t) {               // an expert's last block is half full on average
-        const int64_t blocks = (g.R + g.E * t / 2) / t, least = g.R < g.E ? g.R : g.E;
-        return (blocks > least ? blocks : least) * ((g.N + t - 1) / t);
-    };
-    const int64_t small = tiles(128), rest = small % (2 * cus);
-    const double large = (double)((tiles(256) + cus - 1) / cus);
-    Q8Tiles how = large <= small / (2 * cus) * 0.58 + (rest > cus ? 0.58 : (rest > 0 ? 0.36 : 0)) ? Q8Tiles::LARGE : Q8Tiles::SMALL;
-    if (const char *e = getenv("Q8HOW")) how = (Q8Tiles)atoi(e);
+    const int64_t cus = device_cu_count(), small = tiles_of(g, 128), rest = small % (2 * cus);
+    const double one = (double)((tiles_of(g, 256) + cus - 1) / cus);
+    const double two = (double)(small / (2 * cus)) * 0.58 + (rest > cus ? 0.58 : (rest > 0 ? 0.45 : 0));
+    const double deep = g.K >= 2048 ? (double)((small + cus - 1) / cus) * 0.29 : 1e9;
+    const Q8Tiles how = one <= two && one <= deep ? Q8Tiles::LARGE : (two <= deep ? Q8Tiles::SMALL : Q8Tiles::DEEP);
     if (g.dtype == EMU_F32) return launch_q8_tiles_f32(g, how, s);
     return g.dtype == EMU_BF16 ? launch_q8_tiles_bf16(g, how, s) : launch_q8_tiles_f16(g, how, s);
 }
@@ -89,8 +111,10 @@ hipError_t run_tiles_kernel(const Q8Gemm &g, hipStream_t s) {
 }  // namespace
 
 int launch_q8_gemm(const Q8Gemm &g, hipStream_t s) {
-    const bool few = g.R <= 16 * (int64_t)g.E || g.K == 0 || g.E == 0 || (g.rows && g.xrows == 0);
-    if (few) return api_done(launch_q8_few(g, s), "q8_gemm");
+    // the sums of rows without entries, or without any row to read, are zeros
+    if (g.K == 0 || g.E == 0 || g.xrows == 0) return api_done(launch_q8_few(g, s), "q8_gemm");
+    const double few = time_of_few(g), tiles = time_of_tiles(g);
+    if (few <= tiles) return api_done(launch_q8_few(g, s), "q8_gemm");
     if (fits_tiles(g)) return api_done(run_tiles_kernel(g, s), "q8_gemm");
     // the rows of X through their numbers into the copy, where those are fewer
     const int *const map = g.rows && g.xrows > g.R ? g.rows : nullptr;
@@ -98,9 +122,9 @@ int launch_q8_gemm(const Q8Gemm &g, hipStream_t s) {
     const bool pad = K != g.K, x = pad || !aligned16(g.X) || g.ldx % 16 || (map && g.xrows * g.ldx >= OFFSETS);
     const bool w = pad || !aligned16(g.W) || g.ldw % 16 || g.sw % 16;
     const int mats = g.sw == 0 ? 1 : g.E;                       // one matrix for all experts
-    const Copied cx = {g.X, g.ldx, 0, g.xrows, g.K, map, 1, nullptr, 0, xr, K};
-    const Copied cw = {g.W, g.ldw, g.sw, g.N, g.K, nullptr, mats, g.sw == 0 ? nullptr : g.offsets, g.R, g.N, K};
-    const int64_t xb = x ? up(cx.bytes(), 256) : 0, wb = w ? cw.bytes() : 0;
+    const Copied cx = {g.X, g.ldx, 0, g.xrows, g.K, map, x ? 1 : 0, nullptr, 0, xr, K};
+    const Copied cw = {g.W, g.ldw, g.sw, g.N, g.K, nullptr, w ? mats : 0, g.sw == 0 ? nullptr : g.offsets, g.R, g.N, K};
+    const int64_t xb = up(cx.bytes(), 256), wb = cw.bytes();
     Q8Gemm d = g;
     d.K = (int)K;
     if (x) {
@@ -114,13 +138,12 @@ int launch_q8_gemm(const Q8Gemm &g, hipStream_t s) {
         d.sw = g.sw == 0 ? 0 : cw.rows * K;
     }
     char *at = nullptr;
-    if (fits_tiles(d) && xb + wb <= MOST_COPIED)
+    if (fits_tiles(d) && xb + wb <= MOST_COPIED && 8 + (xb + wb) * 2 / 4e6 + tiles < few)
         if (int rc = api_try_workspace(xb + wb, &at)) return rc;
     if (!at) return api_done(launch_q8_few(g, s), "q8_gemm");
     if (x) d.X = reinterpret_cast<int8_t *>(at);
     if (w) d.W = reinterpret_cast<int8_t *>(at + xb);
-    hipError_t e = x ? copy(cx, at, s) : hipSuccess;
-    if (e == hipSuccess && w) e = copy(cw, at + xb, s);
+    hipError_t e = copy(cx, at, cw, at + xb, s);
     if (e == hipSuccess) e = run_tiles_kernel(d, s);
     return api_done(e, "q8_gemm");
 }

@@ -21,15 +21,27 @@ __device__ __forceinline__ i32x4 mfma16(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
-// Sixteen entries from k on of a row of K, zeros past its end.
+// Sixteen entries from k on of a row of K, zeros past its end: where that is inside of them,
+// the row's last sixteen, moved down.
 __device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K) {
     typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
-    if (k + 16 <= K) return *reinterpret_cast<const unaligned *>(row + k);
+    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
     i32x4 v = {};
+    if (K < 16) {
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-        if (k + j < K) v[j / 4] |= (int)(uint8_t)row[k + j] << (8 * (j % 4));
-    return v;
+        for (int j = 0; j < 16; ++j)
+            if (k + j < K) v[j / 4] |= (int)(uint8_t)row[k + j] << (8 * (j % 4));
+        return v;
+    }
+    const int past = k + 16 - K;
+    v = *reinterpret_cast<const unaligned *>(row + (past > 0 ? K - 16 : k));
+    if (past <= 0) return v;
+    u64x2 u = __builtin_bit_cast(u64x2, v);
+    if (past >= 8) u = u64x2{u[1], 0};
+    const int bits = 8 * (past & 7);
+    u64x2 moved = {u[0] >> bits | (bits > 0 ? u[1] << (64 - bits) : 0), u[1] >> bits};
+    if (past >= 16) moved = u64x2{};
+    return __builtin_bit_cast(i32x4, moved);
 }
 
 template <int N>
@@ -123,7 +135,7 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
 }
 
 template <typename T, int MT, int NT>
-__global__ __launch_bounds__(THREADS, 2) void q8_few_kernel(Q8Gemm g) {
+__global__ __launch_bounds__(THREADS, MT + NT >= 6 ? 2 : 4) void q8_few_kernel(Q8Gemm g) {
     constexpr int COLS = 16 * NT;
     __shared__ int share[WAVES][MT][NT][256];
     const RowTiles tiles(g.offsets, g.E, g.R, 16 * MT, (g.N + COLS - 1) / COLS);
@@ -137,11 +149,30 @@ __global__ __launch_bounds__(THREADS, 2) void q8_few_kernel(Q8Gemm g) {
 
 }  // namespace
 
+// Rows and columns of a tile, in sixteens: rows for those of an expert on average, 64 at most;
+// as many columns as fill the chip (32 rows of 8192 x 4096, 16, 32 and 64 columns: 14.1, 11.5
+// and 14.9 us; 64 rows 23, 16 and 20; 16 rows of 8192 x 8192 18, 20 and 21).
+static int row_sets(const Q8Gemm &g) {
+    return g.R <= 16 * (int64_t)g.E ? 1 : (g.R <= 32 * (int64_t)g.E ? 2 : 4);
+}
+static int64_t expected(const Q8Gemm &g, int nt) {
+    return row_blocks_expected(g.R, g.E, 16 * row_sets(g)) * ((g.N + 16 * nt - 1) / (16 * nt));
+}
+static int column_sets(const Q8Gemm &g) {
+    const int64_t cus = device_cu_count();
+    return expected(g, 4) >= cus ? 4 : (expected(g, 2) >= cus ? 2 : 1);
+}
+
+double q8_few_traffic(const Q8Gemm &g) {
+    const int mt = row_sets(g), nt = column_sets(g);
+    return (double)expected(g, nt) * g.K * 16 * (mt + nt);
+}
+
 hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s) {
     using std::integral_constant;
-    const int mt = g.R <= 16 * (int64_t)g.E ? 1 : 2;
+    // (no expert: rows of zeros)
+    const int mt = g.E > 0 ? row_sets(g) : 4, nt = g.E > 0 ? column_sets(g) : 4;
     auto tiles = [&](int nt) { return row_blocks_bound(g.R, g.E, 16 * mt) * ((g.N + 16 * nt - 1) / (16 * nt)); };
-    const int nt = tiles(4) < device_cu_count() ? 1 : 4;
     with_type(g.dtype, [&](auto z) {
         using T = decltype(z);
         auto run = [&](auto m, auto n) {
@@ -151,10 +182,12 @@ hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s) {
         };
         auto columns = [&](auto m) {
             if (nt == 1) run(m, integral_constant<int, 1>{});
+            else if (nt == 2) run(m, integral_constant<int, 2>{});
             else run(m, integral_constant<int, 4>{});
         };
         if (mt == 1) columns(integral_constant<int, 1>{});
-        else columns(integral_constant<int, 2>{});
+        else if (mt == 2) columns(integral_constant<int, 2>{});
+        else columns(integral_constant<int, 4>{});
     });
     return hipGetLastError();
 }

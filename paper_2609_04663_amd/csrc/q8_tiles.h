@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256, RB * STAGES == 4 ? 2 : 1) void q8_tiles_kernel
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     list.fill(g, Source::TILE);
     Source src(g, list, scales, wave, lane);
-    if (src.start()) run_tiles<i8pair, RB, STAGES>(src, lds, wave);
+    if (src.start()) run_tiles<i8pair, RB, STAGES, RB == 2 ? 2 : 1>(src, lds, wave);
     // rows of no expert
     for (int i = src.i; list.at(i).e == g.E; ++i) {
         const RowTile t = list.at(i);

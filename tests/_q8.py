@@ -65,7 +65,7 @@ def token(x):
 
 def balance(logits, ids, starts):
     """loss, zloss, counts, tokens by the definition, one token at a time, and a bar of
-    zloss: each z is off by the sum's error (64 units of 2^-24, relative, see balance_bar)
+    zloss: each z is off by the sum's error (34 + 36 units of 2^-24, relative, see LOSS_BAR)
     and its own roundings."""
     x = logits.double()
     T, E = x.shape
@@ -80,7 +80,7 @@ def balance(logits, ids, starts):
             p += got[0]
             v = float(got[1])
             z += v * v
-            zb += 2 * abs(v) * (64 + 4 * abs(v)) + 32 * v * v
+            zb += 2 * abs(v) * (70 + 4 * abs(v)) + 32 * v * v
         c = ids[lo:hi].long().reshape(-1)
         c = torch.bincount(c[(c >= 0) & (c < E)], minlength=E)
         C = int(c.sum())
@@ -94,15 +94,17 @@ def balance(logits, ids, starts):
 
 
 # Of the loss, a sum of positive terms, relative: an exponential of a logit at most 16 below
-# the largest is off by 16 + 2 units of 2^-24 (its argument's rounding, its own); the sum of
-# up to 512 (32 to a lane and 4 exchanges) by 18 + 36; the quotient by 2; the sum over a
-# workgroup's tokens by up to 24 additions and 6 exchanges.
-LOSS_BAR = 2.0 ** -24 * (18 + 18 + 36 + 2 + 30 + 2)
+# the largest is off by 16 + 16 + 2 units of 2^-24 (the difference's rounding, that of its
+# product with log2 e, the exponential's own and the constant's); the sum of up to 512 (32 to
+# a lane and 4 exchanges) by that + 36; the quotient by 2; the sum over a workgroup's tokens
+# by up to 24 additions and 6 exchanges.
+LOSS_BAR = 2.0 ** -24 * (34 + 34 + 36 + 2 + 30 + 2)
 
 
 def balance_grad(logits, counts, tokens, dloss, dzloss, starts):
-    """The gradient of the definition and its bar: p is off by 74 units of 2^-24 as above,
-    the mean of the shares by 36 more, z by 64 and its own roundings."""
+    """The gradient of the definition and its bar: p is off by 106 units of 2^-24 as above,
+    the mean of the shares by 106 + 36 more, z by 70 and its own roundings, the products and
+    the difference by 6."""
     x = logits.double()
     T, E = x.shape
     out, bar = torch.zeros((T, E), dtype=torch.float64), torch.zeros((T, E), dtype=torch.float64)
@@ -121,5 +123,5 @@ def balance_grad(logits, counts, tokens, dloss, dzloss, starts):
             p, z = got
             mean = (p * f).sum()
             out[t] = p * (dl * (f - mean) + (dz * z if dz else 0.0))
-            bar[t] = 2.0 ** -24 * 200 * p * (abs(dl) * (f + mean) + (abs(dz) * (1 + abs(z)) if dz else 0.0))
+            bar[t] = 2.0 ** -24 * 260 * p * (abs(dl) * (f + mean) + (abs(dz) * (1 + abs(z)) if dz else 0.0))
     return out, bar
