@@ -3,6 +3,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -110,11 +111,13 @@ __device__ inline int64_t first_tile_of_xcd(const int *__restrict__ offsets, int
 inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
     return R / rows + (E + 1 < R ? E + 1 : R);
 }
-// About so many: an expert's last block is half full on average.
+// Experts that an even load of the rows reaches, and about so many blocks: an expert's
+// last one is half full on average.
+inline double experts_reached(int64_t R, int64_t E) { return E * (1 - pow(1 - 1.0 / E, (double)R)); }
 inline int64_t row_blocks_expected(int64_t R, int64_t E, int64_t rows) {
     if (E == 1) return (R + rows - 1) / rows;
-    const int64_t blocks = (R + E * rows / 2) / rows, least = R < E ? R : E;
-    return blocks > least ? blocks : least;
+    const double reached = experts_reached(R, E), blocks = (R + reached * rows / 2) / rows;
+    return (int64_t)(blocks > reached ? blocks : reached + 0.5);
 }
 
 // A value that all lanes hold, below 2^31, in a scalar register.

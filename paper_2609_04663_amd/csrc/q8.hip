@@ -82,16 +82,18 @@ bool fits_tiles(const Q8Gemm &g) {
 // 8 rows 10 and 16, 32 rows 25 and 19, 128 rows 47 and 38, 4096 rows 144 and 50; 13 of 1501 x 777,
 // 100 rows 15 and 24 (with the copies).
 int64_t tiles_of(const Q8Gemm &g, int64_t t) { return row_blocks_expected(g.R, g.E, t) * ((g.N + t - 1) / t); }
-double matrix_bytes(const Q8Gemm &g) { return (double)(g.R < g.E ? g.R : g.E) * g.N * g.K; }
-// The kernel for few rows: its waves read at 8 TB/s, at half of it from rows that are not
+// The kernel for few rows: its waves read at 7 to 8 TB/s, at half of it from rows that are not
 // multiples of 16 bytes.
-double time_of_few(const Q8Gemm &g) { return 5 + q8_few_traffic(g) / (g.K % 16 == 0 ? 8e6 : 4e6); }
+double time_of_few(const Q8Gemm &g) {
+    return (g.E > 1 ? 8 : 5) + q8_few_traffic(g) / ((g.E > 1 ? 7e6 : 8e6) * (g.K % 16 == 0 ? 1 : 0.5));
+}
 // Tiles of 128 take 0.45 us for a k-block (copies to LDS at 64 bytes a cycle and the reads of
 // fragments), all of them the matrices' bytes at 6 TB/s.
 double time_of_tiles(const Q8Gemm &g) {
     const int64_t cus = device_cu_count(), blocks = (g.K + 127) / 128;
-    const double copies = (double)((tiles_of(g, 128) + cus - 1) / cus) * blocks * 0.45, bytes = matrix_bytes(g) / 6e6;
-    return (g.E > 1 ? 7 : 4) + (copies > bytes ? copies : bytes);
+    const double copies = (g.E > 1 ? 8 : 4) + (double)((tiles_of(g, 128) + cus - 1) / cus) * blocks * 0.45;
+    const double bytes = 1 + experts_reached(g.R, g.E) * g.N * g.K / 6e6;
+    return copies > bytes ? copies : bytes;
 }
 
 // Rounds of one tile of 256 on a CU; of two of 128, 0.58 of that long, or 0.45 where half the
