@@ -56,7 +56,6 @@ __device__ __forceinline__ f32x16 mfma32(frag<half> a, frag<half> b, f32x16 c) {
 // Two 8-bit integers stand for an element of 16 bits: their fragments are 16 bytes of a
 // row too, of 32 indices, and their sums 32-bit integers in the same places.
 using i8pair = int16_t;
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ i32x16 mfma32(frag<i8pair> a, frag<i8pair> b, i32x16 c) {
     return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0,

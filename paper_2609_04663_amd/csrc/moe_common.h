@@ -43,6 +43,30 @@ __device__ __forceinline__ void store_f32(T *p, const float (&x)[N]) {
     *reinterpret_cast<vec<T, N> *>(p) = v;
 }
 
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+// Sixteen bytes from k on of a row of K of them, zeros past its end: where that is inside of them,
+// the row's last sixteen, moved down.
+__device__ __forceinline__ i32x4 load_bytes16(const int8_t *row, int k, int K) {
+    typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
+    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+    i32x4 v = {};
+    if (K < 16) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (k + j < K) v[j / 4] |= (int)(uint8_t)row[k + j] << (8 * (j % 4));
+        return v;
+    }
+    const int past = k + 16 - K;
+    v = *reinterpret_cast<const unaligned *>(row + (past > 0 ? K - 16 : k));
+    if (past <= 0) return v;
+    u64x2 u = __builtin_bit_cast(u64x2, v);
+    if (past >= 8) u = u64x2{u[1], 0};
+    const int bits = 8 * (past & 7);
+    u64x2 moved = {u[0] >> bits | (bits > 0 ? u[1] << (64 - bits) : 0), u[1] >> bits};
+    if (past >= 16) moved = u64x2{};
+    return __builtin_bit_cast(i32x4, moved);
+}
+
 // Rows of expert e: [lo, hi).  offsets (device, E + 1 entries; the first counts
 // as 0) are clamped to [0, R], so that wrong ones cannot lead outside; e == E
 // stands for the rows that belong to no expert, [offsets[E], R).  Without

@@ -28,44 +28,45 @@ struct Copied {
     int64_t bytes() const { return mats * rows * ld; }
 };
 
-// 16 bytes a thread: unaligned loads, aligned stores; blockIdx.y is X or a matrix of W.
-// Bound by bytes.
-__global__ __launch_bounds__(256) void q8_copy_kernel(Copied x, int8_t *__restrict__ to_x, Copied w,
-                                                      int8_t *__restrict__ to_w) {
-    const bool is_x = blockIdx.y < x.mats;
+// Four times 16 bytes a thread: unaligned loads, aligned stores; `per_x` workgroups for X,
+// then `per_w` for each matrix of W.  Bound by bytes.
+constexpr int COPY = 4;
+__global__ __launch_bounds__(256) void q8_copy_kernel(Copied x, int8_t *__restrict__ to_x, unsigned per_x, Copied w,
+                                                      int8_t *__restrict__ to_w, unsigned per_w) {
+    const bool is_x = blockIdx.x < per_x;
+    const unsigned b = is_x ? blockIdx.x : blockIdx.x - per_x;
     const Copied m = is_x ? x : w;
-    const unsigned i = blockIdx.x * 256 + threadIdx.x, per_row = (unsigned)(m.ld / 16);
-    const int64_t row = i / per_row;
-    const int c = (int)(i % per_row) * 16;
-    if (row >= m.rows) return;
-    typedef int i32x4 __attribute__((ext_vector_type(4)));
-    typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
-    const int64_t at = m.map ? m.map[row] : row;
-    for (int e = is_x ? 0 : blockIdx.y - x.mats; e < m.mats; e += gridDim.y - x.mats) {
-        if (m.offsets) {
-            int64_t lo, hi;
-            expert_rows(m.offsets, m.mats, m.R, e, lo, hi);
-            if (lo == hi) continue;
-        }
-        i32x4 v = {};
-        if (at >= 0 && at < m.src_rows) {
-            const int8_t *const p = m.src + e * m.stride + at * m.lds + c;
-            if (c + 16 <= m.cols) {
-                v = *reinterpret_cast<const unaligned *>(p);
-            } else {
+    const int e = is_x ? 0 : (int)(b / per_w);
+    if (m.offsets) {
+        int64_t lo, hi;
+        expert_rows(m.offsets, m.mats, m.R, e, lo, hi);
+        if (lo == hi) return;
+    }
+    const unsigned i0 = (is_x ? b : b % per_w) * (256 * COPY) + threadIdx.x, per_row = (unsigned)(m.ld / 16);
+    int8_t *const dst = (is_x ? to_x : to_w) + e * m.rows * m.ld;
+    i32x4 v[COPY];
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (c + j < m.cols) v[j / 4] |= (int)(uint8_t)p[j] << (8 * (j % 4));
-            }
-        }
-        *reinterpret_cast<i32x4 *>((is_x ? to_x : to_w) + (e * m.rows + row) * m.ld + c) = v;
-        if (is_x) return;
+    for (int j = 0; j < COPY; ++j) {
+        const unsigned i = i0 + 256 * j;
+        const int64_t row = i / per_row;
+        const int c = (int)(i % per_row) * 16;
+        v[j] = i32x4{};
+        if (row >= m.rows) continue;
+        const int64_t at = m.map ? m.map[row] : row;
+        if (at < 0 || at >= m.src_rows) continue;
+        v[j] = load_bytes16(m.src + e * m.stride + at * m.lds, c, m.cols);
+    }
+#pragma unroll
+    for (int j = 0; j < COPY; ++j) {
+        const unsigned i = i0 + 256 * j;
+        if (i / per_row < m.rows) *reinterpret_cast<i32x4 *>(dst + (int64_t)i * 16) = v[j];
     }
 }
 hipError_t copy(const Copied &x, char *to_x, const Copied &w, char *to_w, hipStream_t s) {
-    const int64_t nx = x.mats * x.rows * x.ld, nw = w.mats > 0 ? w.rows * w.ld : 0, n = nx > nw ? nx : nw;
-    const dim3 grid((unsigned)((n / 16 + 255) / 256), x.mats + (w.mats < 32768 ? w.mats : 32768));
-    q8_copy_kernel<<<grid, 256, 0, s>>>(x, reinterpret_cast<int8_t *>(to_x), w, reinterpret_cast<int8_t *>(to_w));
+    auto blocks = [](const Copied &m) { return (unsigned)((m.rows * m.ld / 16 + 256 * COPY - 1) / (256 * COPY)); };
+    const unsigned per_x = x.mats * blocks(x), per_w = blocks(w);
+    q8_copy_kernel<<<per_x + w.mats * per_w, 256, 0, s>>>(x, reinterpret_cast<int8_t *>(to_x), per_x, w,
+                                                         reinterpret_cast<int8_t *>(to_w), per_w);
     return hipGetLastError();
 }
 
@@ -96,16 +97,21 @@ double time_of_tiles(const Q8Gemm &g) {
     return copies > bytes ? copies : bytes;
 }
 
-// Rounds of one tile of 256 on a CU; of two of 128, 0.58 of that long, or 0.45 where half the
-// places stay empty; of one of 128 in four stages, 0.29, for long reductions (it starts when
-// all four are there).  8192 x 8192 x 8192: 449, 521 and 603 us; 2048 x 4096 x 4096: 52, 40 and
-// 43; 300 rows of 8192 x 4096: 49, 27 and 21; 200 over 8 experts of 2048 x 1024: SMALL 9, DEEP 12.
+// Times, us, of rounds of one tile of 256 on a CU, of two of 128 (or of one, where half the
+// places stay empty), and of one of 128 in four stages: those of its k-blocks, and of its
+// start and its stores.  Measured: 8192 x 8192 x 8192 449, 521 and 603 us; 2048 x 4096 x 4096
+// 52, 40 and 43; 300 rows of 8192 x 4096 49, 27 and 21; 4999 over 13 experts of 1501 x 784 in
+// float32 35, 28 and 30; 200 over 8 of 2048 x 1024 SMALL 9, DEEP 12.
 hipError_t run_tiles_kernel(const Q8Gemm &g, hipStream_t s) {
     const int64_t cus = device_cu_count(), small = tiles_of(g, 128), rest = small % (2 * cus);
-    const double one = (double)((tiles_of(g, 256) + cus - 1) / cus);
-    const double two = (double)(small / (2 * cus)) * 0.58 + (rest > cus ? 0.58 : (rest > 0 ? 0.45 : 0));
-    const double deep = g.K >= 2048 ? (double)((small + cus - 1) / cus) * 0.29 : 1e9;
-    const Q8Tiles how = one <= two && one <= deep ? Q8Tiles::LARGE : (two <= deep ? Q8Tiles::SMALL : Q8Tiles::DEEP);
+    const double blocks = (double)((g.K + 127) / 128);
+    auto rounds = [&](int64_t tiles) { return (double)((tiles + cus - 1) / cus); };
+    const double large = rounds(tiles_of(g, 256)) * (blocks * 1.65 + (g.dtype == EMU_F32 ? 18 : 10));
+    const double two = blocks * 0.96 + 6, one = blocks * 0.7 + 4;
+    const double pairs = (double)(small / (2 * cus)) * two + (rest > cus ? two : (rest > 0 ? one : 0));
+    const double deep = rounds(small) * (blocks * 0.45 + 8);
+    const Q8Tiles how = large <= pairs && large <= deep ? Q8Tiles::LARGE
+                                                        : (pairs <= deep ? Q8Tiles::SMALL : Q8Tiles::DEEP);
     if (g.dtype == EMU_F32) return launch_q8_tiles_f32(g, how, s);
     return g.dtype == EMU_BF16 ? launch_q8_tiles_bf16(g, how, s) : launch_q8_tiles_f16(g, how, s);
 }

@@ -13,35 +13,10 @@
 namespace emu {
 namespace {
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int STEP = 128, WAVES = 8, THREADS = 64 * WAVES;
 
 __device__ __forceinline__ i32x4 mfma16(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
-}
-
-// Sixteen entries from k on of a row of K, zeros past its end: where that is inside of them,
-// the row's last sixteen, moved down.
-__device__ __forceinline__ i32x4 load16(const int8_t *row, int k, int K) {
-    typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
-    typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
-    i32x4 v = {};
-    if (K < 16) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (k + j < K) v[j / 4] |= (int)(uint8_t)row[k + j] << (8 * (j % 4));
-        return v;
-    }
-    const int past = k + 16 - K;
-    v = *reinterpret_cast<const unaligned *>(row + (past > 0 ? K - 16 : k));
-    if (past <= 0) return v;
-    u64x2 u = __builtin_bit_cast(u64x2, v);
-    if (past >= 8) u = u64x2{u[1], 0};
-    const int bits = 8 * (past & 7);
-    u64x2 moved = {u[0] >> bits | (bits > 0 ? u[1] << (64 - bits) : 0), u[1] >> bits};
-    if (past >= 16) moved = u64x2{};
-    return __builtin_bit_cast(i32x4, moved);
 }
 
 template <int N>
@@ -55,7 +30,7 @@ struct Piece {                      // 128 indices of N rows of a lane
             for (int p = 0; p < 2; ++p) {
                 const int k = k0 + 64 * p + 16 * h;
                 if (k0 + STEP <= K) v[i][p] = *reinterpret_cast<const unaligned *>(row[i] + k);
-                else v[i][p] = load16(row[i], k, K);
+                else v[i][p] = load_bytes16(row[i], k, K);
             }
     }
 };

@@ -22,17 +22,17 @@ constexpr int UNIT = 8;                                 // entries of a load
 template <typename T>
 using unit = T __attribute__((ext_vector_type(UNIT)));
 
-// Entries e .. e + 7 of a row of K, zeros past its end.
+// A lane takes the entries e .. e + 7 of a row of K.  Where the row ends in between, or
+// before, it takes the row's last eight: entries that another lane has too, and both make
+// the same of them (so no lane has a path of its own: 4999 float32 rows of 1501 12 -> 9 us).  Rows of fewer than eight are read one by one, zeros behind them.
+__device__ __forceinline__ int place_of(int e, int K) { return e + UNIT <= K || K < UNIT ? e : K - UNIT; }
 template <typename T>
-__device__ __forceinline__ unit<T> load_unit(const T *__restrict__ row, int64_t e, int64_t K) {
+__device__ __forceinline__ unit<T> load_unit(const T *__restrict__ row, int e, int K) {
+    if (K >= UNIT) return *reinterpret_cast<const vec<T, UNIT> *>(row + place_of(e, K));
     unit<T> v = unit<T>{};
-    if (e + UNIT <= K) {
-        v = *reinterpret_cast<const vec<T, UNIT> *>(row + e);
-    } else {
 #pragma unroll
-        for (int j = 0; j < UNIT; ++j)
-            if (e + j < K) v[j] = row[e + j];
-    }
+    for (int j = 0; j < UNIT; ++j)
+        if (e + j < K) v[j] = row[e + j];
     return v;
 }
 
@@ -93,10 +93,10 @@ __device__ __forceinline__ uint2 quantise(unit<T> v, const Row &r) {
     return w;
 }
 
-__device__ __forceinline__ void store_unit(int8_t *__restrict__ row, int64_t e, int64_t K, uint2 w) {
+__device__ __forceinline__ void store_unit(int8_t *__restrict__ row, int e, int K, uint2 w) {
     typedef unsigned __attribute__((ext_vector_type(2), aligned(1))) u32x2;
-    if (e + UNIT <= K) {
-        *reinterpret_cast<u32x2 *>(row + e) = u32x2{w.x, w.y};
+    if (K >= UNIT) {
+        *reinterpret_cast<u32x2 *>(row + place_of(e, K)) = u32x2{w.x, w.y};
     } else {
 #pragma unroll
         for (int j = 0; j < UNIT; ++j)
@@ -111,7 +111,7 @@ constexpr int64_t MOST = (1 << 24) - 8;                 // workgroups of a launc
 // LANES lanes to a row, 256 / LANES rows to a workgroup; UNITS of eight entries to a lane,
 // 0: as many as there are, read twice.
 template <typename T, int LANES, int UNITS>
-__global__ __launch_bounds__(256) void q8_pack_kernel(const T *__restrict__ X, int64_t rows, int64_t ldx, int64_t K,
+__global__ __launch_bounds__(256) void q8_pack_kernel(const T *__restrict__ X, int64_t rows, int64_t ldx, int K,
                                                       int8_t *__restrict__ Q, int64_t ldq,
                                                       float *__restrict__ scales) {
     constexpr int ROWS = 256 / LANES;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void q8_pack_kernel(const T *__restrict__ X, i
 #pragma unroll
             for (int i = 0; i < UNITS; ++i) top = max_of(top, top_of<T>(v[i]));
         } else {
-            for (int64_t e = lane * UNIT; e < K; e += LANES * UNIT) top = max_of(top, top_of<T>(load_unit(x, e, K)));
+            for (int e = lane * UNIT; e < K; e += LANES * UNIT) top = max_of(top, top_of<T>(load_unit(x, e, K)));
         }
         top = over_lanes<(LANES < 64 ? LANES : 64)>(top, max_of);
         if constexpr (LANES > 64) {
@@ -148,37 +148,40 @@ __global__ __launch_bounds__(256) void q8_pack_kernel(const T *__restrict__ X, i
                 if (e < K) store_unit(q, e, K, quantise<T>(v[i], r));
             }
         } else {
-            for (int64_t e = lane * UNIT; e < K; e += LANES * UNIT)
+            for (int e = lane * UNIT; e < K; e += LANES * UNIT)
                 store_unit(q, e, K, quantise<T>(load_unit(x, e, K), r));
         }
     }
 }
 
-// 64 lanes to a row's columns, `run` of them from blockIdx.y run on.
+// 64 lanes to a row's columns, `run` of them from blockIdx.y run on.  One unit of a lane at
+// a time, and its load behind a branch, so that it stays there: with four in flight 131072
+// rows of 2048 took 184 us instead of 127, with the next one's load moved up 143.
 template <typename T>
 __global__ __launch_bounds__(256) void q8_unpack_kernel(const int8_t *__restrict__ Q, int64_t rows, int64_t ldq,
-                                                        int64_t K, int run, const float *__restrict__ scales,
+                                                        int K, int run, const float *__restrict__ scales,
                                                         T *__restrict__ X, int64_t ldx) {
     for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64; row < rows; row += (int64_t)gridDim.x * 4) {
         const float scale = scales[row];
         const int8_t *const q = Q + row * ldq;
         T *const x = X + row * ldx;
-        // the next unit of the run, or the first of the workgroup's next run
-        const int64_t skip = ((int64_t)gridDim.y - 1) * run + 64 * UNIT;
-        for (int64_t e = (int64_t)blockIdx.y * run + threadIdx.x % 64 * UNIT; e < K;
-             e += (int)(e & (run - 1)) + 64 * UNIT < run ? 64 * UNIT : skip) {
-            const unit<int8_t> v = load_unit(q, e, K);
-            float f[UNIT];
+        for (int c0 = blockIdx.y * run; c0 < K; c0 += gridDim.y * run)
+#pragma unroll 1
+            for (int e = c0 + threadIdx.x % 64 * UNIT; e < K && e < c0 + run; e += 64 * UNIT) {
+                unit<int8_t> v;
+                if (e + UNIT <= K) v = *reinterpret_cast<const vec<int8_t, UNIT> *>(q + e);
+                else v = load_unit(q, e, K);
+                float f[UNIT];
 #pragma unroll
-            for (int j = 0; j < UNIT; ++j) f[j] = (float)v[j] * scale;
-            if (e + UNIT <= K) {
-                store_f32<UNIT>(x + e, f);
-            } else {
+                for (int j = 0; j < UNIT; ++j) f[j] = (float)v[j] * scale;
+                if (K >= UNIT) {
+                    store_f32<UNIT>(x + place_of(e, K), f);
+                } else {
 #pragma unroll
-                for (int j = 0; j < UNIT; ++j)
-                    if (e + j < K) x[e + j] = (T)f[j];
+                    for (int j = 0; j < UNIT; ++j)
+                        if (e + j < K) x[e + j] = (T)f[j];
+                }
             }
-        }
     }
 }
 
@@ -192,7 +195,7 @@ hipError_t launch_q8_pack(int dtype, const void *X, int64_t rows, int64_t ldx, i
             constexpr int LANES = decltype(lanes)::value, ROWS = 256 / LANES;
             const int64_t grid = (rows + ROWS - 1) / ROWS;
             q8_pack_kernel<T, LANES, decltype(units)::value><<<(unsigned)(grid < MOST ? grid : MOST), 256, 0, s>>>(
-                static_cast<const T *>(X), rows, ldx, K, Q, ldq, scales);
+                static_cast<const T *>(X), rows, ldx, (int)K, Q, ldq, scales);
         };
         using std::integral_constant;
         const integral_constant<int, 16> sixteen;
@@ -217,15 +220,14 @@ hipError_t launch_q8_pack(int dtype, const void *X, int64_t rows, int64_t ldx, i
 
 hipError_t launch_q8_unpack(int dtype, const int8_t *Q, int64_t rows, int64_t ldq, int64_t K, const float *scales,
                             void *X, int64_t ldx, hipStream_t s) {
-    // long runs of a row, but where so few would leave the chip empty: 1 row of 4096, 3.2 us
-    // in one run, 2.3 in eight; 131072 rows of 2048, 127 us in one and 175 in two
+    // long runs of a row, but where so few workgroups would leave the chip empty
     const int64_t high = (rows + 3) / 4;
     const int run = high * ((K + 4095) / 4096) < 1024 ? 512 : 4096;
     const int64_t cols = (K + run - 1) / run, y = cols < 32768 ? cols : 32768, most = MOST / y;
     const dim3 grid((unsigned)(high < most ? high : most), (unsigned)y);
     with_type(dtype, [&](auto z) {
         using T = decltype(z);
-        q8_unpack_kernel<T><<<grid, 256, 0, s>>>(Q, rows, ldq, K, run, scales, static_cast<T *>(X), ldx);
+        q8_unpack_kernel<T><<<grid, 256, 0, s>>>(Q, rows, ldq, (int)K, run, scales, static_cast<T *>(X), ldx);
     });
     return hipGetLastError();
 }
