@@ -630,6 +630,11 @@ def _int8_mat(t, name: str):
     return _layout(t, torch.int8, name)
 
 
+def _shaped(t, dtype):
+    """A contiguous tensor of t's shape (empty_like is the cheapest)."""
+    return torch.empty_like(t, dtype=dtype) if t.is_contiguous() else t.new_empty(t.shape, dtype=dtype)
+
+
 def _code_of(dtype) -> int:
     code = _DTYPES.get(dtype)
     if code is None:
@@ -646,8 +651,7 @@ def q8_pack(X: torch.Tensor):
     flat = X if X.dim() == 2 else X.reshape(lead.numel(), K)
     code = _float_mat(flat, "X")
     _same_gpu(("X", X))
-    Q = torch.empty(X.shape, dtype=torch.int8, device=X.device)
-    scales = torch.empty(lead, dtype=torch.float32, device=X.device)
+    Q, scales = _shaped(X, torch.int8), X.new_empty(lead, dtype=torch.float32)
     _launch(lib().emu_q8_pack, X.device, code, flat.shape[0], K, flat.data_ptr(), _ld(flat), Q.data_ptr(),
             max(1, K), scales.data_ptr())
     return Q, scales
@@ -663,7 +667,7 @@ def q8_unpack(Q, scales, dtype=torch.bfloat16) -> torch.Tensor:
     _int8_mat(flat, "Q")
     _packed(scales, "scales", torch.float32, lead)
     _same_gpu(("Q", Q), ("scales", scales))
-    X = torch.empty(Q.shape, dtype=dtype, device=Q.device)
+    X = _shaped(Q, dtype)
     _launch(lib().emu_q8_unpack, Q.device, code, flat.shape[0], K, flat.data_ptr(), _ld(flat),
             scales.data_ptr(), X.data_ptr(), max(1, K))
     return X
@@ -676,7 +680,11 @@ def q8_gemm(X, xscales, W, wscales, offsets=None, rows=None, dtype=torch.bfloat1
     _int8_mat(X, "X")
     if not isinstance(W, torch.Tensor) or W.dim() not in (2, 3):
         raise ValueError("W must be a 2-D or 3-D tensor")
-    E, N, K, ldw, stride = _experts(W if W.dim() == 3 else W[None], "W", torch.int8)
+    if W.dtype is torch.int8 and W.is_contiguous():
+        E, N, K = (1, *W.shape) if W.dim() == 2 else W.shape
+        ldw, stride = max(1, K), N * K
+    else:
+        E, N, K, ldw, stride = _experts(W if W.dim() == 3 else W[None], "W", torch.int8)
     if X.shape[1] != K:
         raise ValueError("inner dimensions differ")
     if offsets is None and E != 1:
@@ -686,7 +694,7 @@ def q8_gemm(X, xscales, W, wscales, offsets=None, rows=None, dtype=torch.bfloat1
     R = _grouping(X, offsets, rows, E)
     if Y is None:
         code = _code_of(dtype)
-        Y = torch.empty((R, N), dtype=dtype, device=X.device)
+        Y = X.new_empty((R, N), dtype=dtype)
     else:
         code = _float_mat(Y, "Y")
         if tuple(Y.shape) != (R, N):

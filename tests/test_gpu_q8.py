@@ -6,6 +6,7 @@ import torch
 
 import _moe as M
 import _q8 as Q
+import _q8_shapes as S
 
 pytestmark = pytest.mark.gpu
 
@@ -148,24 +149,14 @@ def _check(emu, X, xs, W, ws, offsets, rows, dt, X_=None, W_=None):
     return got
 
 
-# rows, experts, N, K: few rows of each expert, one and two tiles of 16, one and four tiles of
-# columns; more of them on tiles of 128 and 256, K in whole and broken k-blocks and chunks
-FEW = [(1, 1, 1, 1), (1, 1, 300, 77), (3, 1, 65, 128), (16, 1, 4096, 200), (16, 1, 20000, 130), (7, 3, 129, 16),
-       (40, 20, 70, 1100), (300, 30, 1000, 257), (9, 1, 33, 5000)]
-SHAPES = [(17, 1, 128, 16), (130, 1, 130, 48), (200, 2, 257, 112), (300, 3, 100, 128), (260, 1, 513, 144),
-          (500, 4, 128, 240), (1000, 3, 300, 256), (700, 7, 200, 272), (129, 1, 1000, 1040), (2000, 5, 1024, 400),
-          (4100, 3, 1500, 640), (3000, 40, 520, 384)]
-ODD = [(100, 1, 130, 1), (300, 3, 257, 77), (1000, 5, 129, 1001), (2500, 2, 700, 333)]
-
-
 @pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("kind", list(M.TYPES))
-@pytest.mark.parametrize("R,E,N,K", FEW + SHAPES + ODD)
+@pytest.mark.parametrize("R,E,N,K", S.FEW + S.SHAPES + S.ODD)
 def test_product(emu, kind, R, E, N, K, gather):
     _check(emu, *_operands(R + N + K, R, E, N, K, gather), M.TYPES[kind])
 
 
-@pytest.mark.parametrize("R,E,N,K", [(33000, 3, 1030, 144), (20000, 70, 2048, 128), (16000, 1, 4100, 400)])
+@pytest.mark.parametrize("R,E,N,K", S.LARGE)
 def test_large_product(emu, R, E, N, K):
     """More tiles than workgroups; compared on the GPU in 64 bits."""
     X, xs, W, ws, offsets, rows = _operands(R, R, E, N, K, True)
@@ -302,3 +293,82 @@ def test_in_a_graph(emu, K):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
+
+
+@pytest.mark.parametrize("K,lead", [(1001, 0), (1008, 1)])
+def test_few_of_many_rows_through_a_copy(emu, K, lead):
+    """Rows of X that are not multiples of 16 bytes, of which the product reads fewer than X has:
+    they are copied in order, their scales still by their numbers."""
+    gen = torch.Generator().manual_seed(K)
+    R, T, E, N = 3000, 9000, 2, 700
+    whole = torch.randint(-128, 128, (T * K + lead,), generator=gen, dtype=torch.int8)
+    X = whole[lead:].view(T, K)
+    W = torch.randint(-128, 128, (E, N, K), generator=gen, dtype=torch.int8)
+    xs, ws = torch.rand(T, generator=gen) * 0.01, torch.rand((E, N), generator=gen) * 0.01
+    rows = torch.randint(-5, T + 5, (R,), generator=gen).int()
+    offsets = torch.tensor([0, 1700, 2900], dtype=torch.int32)
+    _check(emu, X, xs, W, ws, offsets, rows, torch.float32, whole.cuda()[lead:].view(T, K))
+
+
+def test_many_odd_rows_without_workspace(emu):
+    """A captured call that finds no workspace reads the operands as they are."""
+    X, xs, W, ws, offsets, rows = _operands(3, 2500, 3, 300, 515, True)
+    ref = Q.product(X, xs, W, ws, offsets, rows)
+    args = [t.cuda() for t in (X, xs, W, ws, offsets, rows)]
+    eager = emu.q8_gemm(*args)
+    torch.cuda.synchronize()
+    emu.release_workspace()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = emu.q8_gemm(*args)
+    assert emu.workspace_bytes() == 0
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        M.check(out, ref, Q.product_bar(ref, torch.bfloat16))
+    M.check(eager, ref, Q.product_bar(ref, torch.bfloat16))
+
+
+def test_on_another_stream(emu):
+    """Work of one stream, results read on it after a synchronisation; two streams in turn."""
+    gen = torch.Generator().manual_seed(12)
+    x = torch.randn((700, 333), generator=gen).cuda()
+    w = torch.randn((2, 500, 333), generator=gen).cuda()
+    offsets = torch.tensor([0, 300, 700], dtype=torch.int32).cuda()
+    ref = None
+    torch.cuda.synchronize()
+    for stream in (torch.cuda.Stream(), torch.cuda.current_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(stream):
+            q, s = emu.q8_pack(x)
+            out = emu.q8_gemm(q, s, *emu.q8_pack(w), offsets)
+            stream.synchronize()
+        ref = out.clone() if ref is None else ref
+        assert torch.equal(out, ref)
+
+
+def test_the_run_of_them(emu):
+    """Routed, packed, multiplied, activated, packed, multiplied, combined, as the example
+    serves a layer; every step against its own plain form on the same inputs."""
+    gen = torch.Generator().manual_seed(9)
+    T, D, H, E, k = 50, 192, 320, 8, 2
+    x = torch.randn((T, D), generator=gen).to(torch.bfloat16).cuda()
+    W1, W2 = (torch.randn(s, generator=gen).to(torch.bfloat16).cuda() / 10 for s in ((E, H, D), (E, D, H)))
+    r = emu.moe_route(torch.randn((T, E), generator=gen).cuda(), k)
+    p1, p2 = emu.q8_pack(W1), emu.q8_pack(W2)
+    q, s = emu.q8_pack(x)
+    h = emu.q8_gemm(q, s, *p1, r.offsets, r.rows)
+    ref = Q.product(q.cpu(), s.cpu(), p1[0].cpu(), p1[1].cpu(), r.offsets.cpu(), r.rows.cpu())
+    M.check(h, ref, Q.product_bar(ref, torch.bfloat16))
+    a = torch.nn.functional.silu(h)
+    q, s = emu.q8_pack(a)
+    assert torch.equal(q.cpu(), Q.pack(a.cpu())[0])
+    z = emu.q8_gemm(q, s, *p2, r.offsets)
+    ref = Q.product(q.cpu(), s.cpu(), p2[0].cpu(), p2[1].cpu(), r.offsets.cpu(), None)
+    M.check(z, ref, Q.product_bar(ref, torch.bfloat16))
+    y = emu.moe_combine(z, r.slots, r.weights)
+    # against 16-bit products: each packing is off by half a 127th of a row's largest entry, 0.4 %
+    # of it, some 1.2 % of a typical one; four packings, which add up at random
+    full = emu.moe_combine(emu.grouped_gemm(torch.nn.functional.silu(
+        emu.grouped_gemm(x, W1, r.offsets, transb="T", rows=r.rows)), W2, r.offsets, transb="T"), r.slots, r.weights)
+    assert float((y.float() - full.float()).norm() / full.float().norm()) < 0.05
