@@ -1,5 +1,5 @@
-"""A mixture-of-experts layer from the library's operators: trained for a few steps,
-then served token by token from 4-bit matrices.
+"""A mixture-of-experts layer from the library's operators: trained for a few steps with
+a balance loss, then served token by token from 4-bit matrices, and in a batch from 8 bits.
 
     python examples/moe_layer.py
 
@@ -8,6 +8,7 @@ then served token by token from 4-bit matrices.
     h = W1[expert] x                       grouped_gemm, rows gathered through the order
     z = W2[expert] silu(h)                 grouped_gemm
     y = sum of weights z                   moe_combine
+    loss, z loss                           moe_balance
 
 The matrices of the experts are stored E x out x in (transb 'T'), as q4_pack wants
 them.  Everything is ordered on torch's current stream and nothing waits for the
@@ -24,7 +25,7 @@ import paper_2609_04663_amd as emu  # noqa: E402
 
 class MoE(torch.autograd.Function):
     """y of tokens x (T x D) for the router Wr (D x E, float32) and the experts'
-    W1 (E x H x D) and W2 (E x D x H), k experts a token."""
+    W1 (E x H x D) and W2 (E x D x H), k experts a token; the router's losses."""
 
     @staticmethod
     def forward(ctx, x, Wr, W1, W2, k, scope):
@@ -33,14 +34,17 @@ class MoE(torch.autograd.Function):
         h = emu.grouped_gemm(x, W1, r.offsets, transb="T", rows=r.rows)
         a = torch.nn.functional.silu(h)
         z = emu.grouped_gemm(a, W2, r.offsets, transb="T")
-        ctx.save_for_backward(x, Wr, W1, W2, logits, h, a, z, *r)
+        b = emu.moe_balance(logits, r.ids)
+        ctx.save_for_backward(x, Wr, W1, W2, logits, h, a, z, b.counts, b.tokens, *r)
         ctx.scope = scope
-        return emu.moe_combine(z, r.slots, r.weights)
+        ctx.set_materialize_grads(False)
+        return emu.moe_combine(z, r.slots, r.weights), b.loss, b.zloss
 
     @staticmethod
-    def backward(ctx, dy):
-        x, Wr, W1, W2, logits, h, a, z, *r = ctx.saved_tensors
+    def backward(ctx, dy, dloss, dzloss):
+        x, Wr, W1, W2, logits, h, a, z, counts, tokens, *r = ctx.saved_tensors
         r = emu.Routing(*r)
+        dy = x.new_zeros(x.shape) if dy is None else dy
         dz, dweights = emu.moe_combine_grad(dy.contiguous(), z, r.slots, r.weights, r.rows)
         dW2 = emu.grouped_wgrad(a, dz, r.offsets, transb="T")
         da = emu.grouped_gemm(dz, W2, r.offsets)
@@ -49,13 +53,21 @@ class MoE(torch.autograd.Function):
         dW1 = emu.grouped_wgrad(x, dh, r.offsets, transb="T", rows=r.rows)
         dx = emu.moe_combine(emu.grouped_gemm(dh, W1, r.offsets), r.slots)     # each token's rows
         dlogits = emu.moe_route_grad(logits, r.ids, r.weights, dweights, ctx.scope)
+        if dloss is not None or dzloss is not None:
+            dloss = counts.new_zeros(1, dtype=torch.float32) if dloss is None else dloss
+            dlogits = dlogits + emu.moe_balance_grad(logits, counts, tokens, dloss, dzloss)
         dWr = emu.sgemm_ex(x.float(), dlogits, transa="T")
         dx = dx + emu.sgemm_ex(dlogits, Wr, transb="T").to(dx.dtype)
         return dx, dWr, dW1, dW2, None, None
 
 
-def moe(x, Wr, W1, W2, k, scope="chosen"):
+def moe_with_losses(x, Wr, W1, W2, k, scope="chosen"):
+    """y, the balance loss and the squared log of the router's softmax sum (one each)."""
     return MoE.apply(x, Wr, W1, W2, k, scope)
+
+
+def moe(x, Wr, W1, W2, k, scope="chosen"):
+    return moe_with_losses(x, Wr, W1, W2, k, scope)[0]
 
 
 class Served:
@@ -72,6 +84,21 @@ class Served:
         return emu.moe_combine(z, r.slots, r.weights)
 
 
+class Served8:
+    """The layer with the experts' matrices and each product's rows in 8 bits, for a prompt's
+    tokens."""
+
+    def __init__(self, Wr, W1, W2, k, scope="chosen"):
+        self.Wr, self.k, self.scope = Wr, k, scope
+        self.W1, self.W2 = emu.q8_pack(W1), emu.q8_pack(W2)
+
+    def __call__(self, x):
+        r = emu.moe_route(emu.sgemm(x.float(), self.Wr), self.k, self.scope)
+        h = emu.q8_gemm(*emu.q8_pack(x), *self.W1, r.offsets, r.rows, dtype=x.dtype)
+        z = emu.q8_gemm(*emu.q8_pack(torch.nn.functional.silu(h)), *self.W2, r.offsets, dtype=x.dtype)
+        return emu.moe_combine(z, r.slots, r.weights)
+
+
 def main(T=4096, D=1024, H=512, E=32, k=4, steps=20, dtype=torch.bfloat16):
     gen = torch.Generator(device="cuda").manual_seed(0)
 
@@ -84,19 +111,22 @@ def main(T=4096, D=1024, H=512, E=32, k=4, steps=20, dtype=torch.bfloat16):
     masters = [w.requires_grad_() for w in (Wr, W1, W2)]
     opt = torch.optim.Adam(masters, lr=2e-3)
     for step in range(steps):
-        y = moe(x, Wr, W1.to(dtype), W2.to(dtype), k)
+        y, balance, zloss = moe_with_losses(x, Wr, W1.to(dtype), W2.to(dtype), k)
         loss = ((y.float() - target) ** 2).mean()
         opt.zero_grad()
-        loss.backward()
+        (loss + 0.01 * balance.sum() + 1e-4 * zloss.sum()).backward()
         opt.step()
         if step % 5 == 0 or step == steps - 1:
-            print(f"step {step:3d}  loss {loss.item():.4f}", flush=True)
+            print(f"step {step:3d}  loss {loss.item():.4f}  balance {balance.item():.3f}", flush=True)
     with torch.no_grad():
         W1, W2 = W1.to(dtype), W2.to(dtype)
         served = Served(Wr, W1, W2, k)
         exact = moe(x[:16], Wr, W1, W2, k).float()
         off = torch.cat([served(x[t:t + 1]).float() for t in range(16)]) - exact
         print(f"served from 4 bits, token by token: relative difference {(off.norm() / exact.norm()).item():.3f}")
+        exact = moe(x, Wr, W1, W2, k).float()
+        off = Served8(Wr, W1, W2, k)(x).float() - exact
+        print(f"served from 8 bits, all tokens: relative difference {(off.norm() / exact.norm()).item():.3f}")
     return loss.item()
 
 
