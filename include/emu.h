@@ -210,8 +210,9 @@ int emu_set_fallback(int mode);
 int emu_set_sgemm_split(int mode);
 
 /* ---------------------------------------------------------------------------
-   Operators of a mixture-of-experts layer: the router, the products with the
-   experts' matrices (forward and gradients) and with 4-bit expert matrices.
+   Operators of a mixture-of-experts layer: the router and its balance loss, the products with
+   the experts' matrices (forward and gradients), with 4-bit expert matrices, and of rows and
+   matrices in 8-bit integers.
 
    Common to them.  A token t chooses k of E experts; the (token, choice) pairs
    ordered by expert, then token, are the rows.  Element types are EMU_F32,
@@ -224,10 +225,11 @@ int emu_set_sgemm_split(int mode);
    Matrices are row-major with leading dimensions in elements, at any element's
    alignment; index arrays are int32.  Device pointers, ordered on the current
    stream, no host synchronisation (but where the workspace grows).  It is used by emu_moe_route
-   (more than 64 tokens), emu_q4_gemm (a reduction that is split) and the
-   grouped products (16-bit operands that are copied to 16-byte alignment first,
-   sums of few matrices in pieces); the last three do without it where it cannot
-   grow (no memory beside what is held, EMU_WORKSPACE_LIMIT, a stream under capture).
+   (more than 64 tokens), emu_moe_balance (more than 256), emu_q4_gemm (a reduction that is
+   split), the grouped products (16-bit operands that are copied to 16-byte alignment first,
+   sums of few matrices in pieces) and emu_q8_gemm (operands that are copied); all but the first
+   two do without it where it cannot grow (no memory beside what is held, EMU_WORKSPACE_LIMIT, a
+   stream under capture).
    offsets: E + 1 entries, rows [offsets[e], offsets[e + 1]) belong to expert e
    (offsets[0] counts as 0); an expert may have none.  Rows from offsets[E] on
    belong to no expert: their outputs are zero and their inputs are not used.
