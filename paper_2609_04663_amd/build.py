@@ -24,7 +24,7 @@ SOURCES = ["split.hip", "gemm_f32.hip", "gemm_f64.hip", "gemm_f64s.hip", "gemm_f
            "grouped_few.hip", "grouped_staged_f32.hip", "grouped_staged_bf16.hip",
            "grouped_staged_f16.hip", "q4.hip", "q4_f32.hip", "q4_bf16.hip", "q4_f16.hip",
            "moe_balance.hip", "q8_pack.hip", "q8.hip", "q8_few.hip", "q8_tiles_f32.hip",
-           "q8_tiles_bf16.hip", "q8_tiles_f16.hip", "moe_api.hip"]
+           "q8_tiles_bf16.hip", "q8_tiles_f16.hip", "q8_tiles_sums.hip", "moe_api.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

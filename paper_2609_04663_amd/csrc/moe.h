@@ -126,10 +126,21 @@ struct Q8Gemm {
     int64_t ldx, ldw, sw, ldy;
     const int *offsets, *rows;
     const int *scaled;              // rows of X that the rows of Y have their scales from: `rows`, also where X is in order
+    // Sums: split i of the launch (blockIdx.y) takes the indices i part .. (i + 1) part - 1 and
+    // writes its 32-bit sums, without scales, to Y + i R ldy.
+    int part;
 };
 int launch_q8_gemm(const Q8Gemm &g, hipStream_t s);
 hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s);
-double q8_few_traffic(const Q8Gemm &g);     // bytes that its waves read, of X and W (E > 0)
+hipError_t launch_q8_few_sums(const Q8Gemm &g, int splits, hipStream_t s);
+// What its time goes by (E > 0): its tiles, their rows and columns in sixteens; indices that
+// a workgroup takes at a time.
+struct Q8FewShape {
+    double tiles;
+    int mt, nt;
+};
+Q8FewShape q8_few_shape(const Q8Gemm &g);
+constexpr int Q8_FEW_ROUND = 1024;
 // The kernel of operands copied straight to LDS (q8_tiles.h), with square output tiles of 256,
 // or of 128, two workgroups of two stages on a CU or one of four; one source file for each
 // type of Y: they take long to compile.
@@ -137,5 +148,6 @@ enum class Q8Tiles { LARGE, SMALL, DEEP };
 hipError_t launch_q8_tiles_f32(const Q8Gemm &g, Q8Tiles how, hipStream_t s);
 hipError_t launch_q8_tiles_bf16(const Q8Gemm &g, Q8Tiles how, hipStream_t s);
 hipError_t launch_q8_tiles_f16(const Q8Gemm &g, Q8Tiles how, hipStream_t s);
+hipError_t launch_q8_tiles_sums(const Q8Gemm &g, int splits, hipStream_t s);    // DEEP
 
 }  // namespace emu

@@ -286,7 +286,7 @@ int emu_q8_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, const int8_t 
     api_clear_error();
     if (R == 0 || N == 0) return EMU_OK;
     const Q8Gemm g = {dtype, E, (int)N, (int)K, R, XR, X, W, xscales, wscales, Y, ldx, ldw, stride, ldy, offsets,
-                      rows, rows};
+                      rows, rows, (int)K};
     return launch_q8_gemm(g, api_stream());
 }
 

@@ -191,6 +191,16 @@ __device__ __forceinline__ float exp_below(float x, float m) {
     return x == m ? 1.0f : (x > -INFINITY ? expf(x - m) : 0.0f);
 }
 
+// The operands and sums of the workgroup's split (see Q8Gemm::part).
+template <typename Gemm>
+__device__ __forceinline__ void to_split(Gemm &g) {
+    const int i = blockIdx.y, first = i * g.part;
+    g.X += first;
+    g.W += first;
+    g.K = g.K - first < g.part ? g.K - first : g.part;
+    g.Y = static_cast<int *>(g.Y) + i * g.R * g.ldy;
+}
+
 // A workgroup's block of rows and its column tile.
 struct RowTile {
     int e;                 // expert; -1: there is no such tile; E: rows of no expert

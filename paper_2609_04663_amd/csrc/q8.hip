@@ -83,18 +83,49 @@ bool fits_tiles(const Q8Gemm &g) {
 // 8 rows 10 and 16, 32 rows 25 and 19, 128 rows 47 and 38, 4096 rows 144 and 50; 13 of 1501 x 777,
 // 100 rows 15 and 24 (with the copies).
 int64_t tiles_of(const Q8Gemm &g, int64_t t) { return row_blocks_expected(g.R, g.E, t) * ((g.N + t - 1) / t); }
-// The kernel for few rows: its waves read at 7 to 8 TB/s, at half of it from rows that are not
-// multiples of 16 bytes.
-double time_of_few(const Q8Gemm &g) {
-    return (g.E > 1 ? 8 : 5) + q8_few_traffic(g) / ((g.E > 1 ? 7e6 : 8e6) * (g.K % 16 == 0 ? 1 : 0.5));
+// The kernel for few rows: its waves read X and W at 7 to 8 TB/s, at half of it from rows that
+// are not multiples of 16 bytes, the matrices come at 6 TB/s; a workgroup takes 1024 indices
+// in 0.7 to 2.5 us, by its loads; the largest tiles are alone on a CU and take 6 us beside.
+double time_of_few(const Q8Gemm &g, int splits = 1) {
+    const Q8FewShape f = q8_few_shape(g);
+    const double cus = (double)device_cu_count(), loads = f.mt + f.nt, aligned = g.K % 16 == 0 ? 1 : 0.5;
+    const double rounds = (double)(up(g.K, Q8_FEW_ROUND * splits) / (Q8_FEW_ROUND * splits));
+    double t = (0.1 + 0.3 * loads) * rounds * ceil(f.tiles * splits / (2 * cus));
+    t = fmax(t, f.tiles * g.K * 16 * loads / ((g.E > 1 ? 7e6 : 8e6) * aligned));
+    t = fmax(t, experts_reached(g.R, g.E) * g.N * g.K / (6e6 * aligned));
+    return (g.E > 1 ? 8 : 5) + t + (loads == 8 ? f.tiles * splits / cus * 6 : 0);
 }
 // Tiles of 128 take 0.45 us for a k-block (copies to LDS at 64 bytes a cycle and the reads of
 // fragments), all of them the matrices' bytes at 6 TB/s.
-double time_of_tiles(const Q8Gemm &g) {
-    const int64_t cus = device_cu_count(), blocks = (g.K + 127) / 128;
-    const double copies = (g.E > 1 ? 8 : 4) + (double)((tiles_of(g, 128) + cus - 1) / cus) * blocks * 0.45;
+double time_of_tiles(const Q8Gemm &g, int splits = 1) {
+    const int64_t cus = device_cu_count(), blocks = ((g.K + 127) / 128 + splits - 1) / splits;
+    const double copies =
+        (g.E > 1 || splits > 1 ? 8 : 4) + (double)((tiles_of(g, 128) * splits + cus - 1) / cus) * blocks * 0.45;
     const double bytes = 1 + experts_reached(g.R, g.E) * g.N * g.K / 6e6;
     return copies > bytes ? copies : bytes;
+}
+// Sums of splits of a long reduction: written, read and joined at 4.5 TB/s by a kernel of
+// its own, one launch more.
+double time_of_join(const Q8Gemm &g, int splits) { return 7 + (double)g.R * g.N * 8 * splits / 4.5e6; }
+
+// Y from the sums of the splits (R x ld each): one matrix, four columns to a thread.
+template <typename T>
+__global__ __launch_bounds__(256) void q8_join_kernel(Q8Gemm g, const int *__restrict__ sums, int64_t ld,
+                                                      int splits) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, per_row = ld / 4, r = i / per_row;
+    const int c = (int)(i - r * per_row) * 4;
+    if (r >= g.R) return;
+    int64_t lo, hi;
+    expert_rows(g.offsets, 1, g.R, 0, lo, hi);
+    const int64_t at = g.rows ? g.rows[r] : r;
+    const bool there = r < hi && at >= 0 && at < g.xrows;
+    i32x4 sum = {};
+    for (int k = 0; k < splits; ++k) sum += *reinterpret_cast<const i32x4 *>(sums + (k * g.R + r) * ld + c);
+    const double x = there ? g.xs[at] : 0.0;
+    T *const y = static_cast<T *>(g.Y) + r * g.ldy + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (c + j < g.N) y[j] = there ? (T)(float)((double)sum[j] * g.ws[c + j] * x) : (T)0.0f;
 }
 
 // Times, us, of rounds of one tile of 256 on a CU, of two of 128 (or of one, where half the
@@ -118,41 +149,105 @@ hipError_t run_tiles_kernel(const Q8Gemm &g, hipStream_t s) {
 
 }  // namespace
 
-int launch_q8_gemm(const Q8Gemm &g, hipStream_t s) {
-    // the sums of rows without entries, or without any row to read, are zeros
-    if (g.K == 0 || g.E == 0 || g.xrows == 0) return api_done(launch_q8_few(g, s), "q8_gemm");
-    const double few = time_of_few(g), tiles = time_of_tiles(g);
-    if (few <= tiles) return api_done(launch_q8_few(g, s), "q8_gemm");
-    if (fits_tiles(g)) return api_done(run_tiles_kernel(g, s), "q8_gemm");
+// A product of one matrix whose reduction is split, if that is faster than `time` us: *done,
+// or else nothing was launched.
+// 294 rows of 2176 x 8128: 33 us in one piece, 23 in four; 512 of 4096 x 16384 59 and, in two,
+// 49; 39 of 64 x 6656 16 and, in four, 11; 16 of 2048 x 16384 17 and, in 16, 23.
+static int split_gemm(const Q8Gemm &g, double time, hipStream_t s, bool *done) {
+    *done = false;
+    if (g.E != 1) return EMU_OK;
+    const bool fits = fits_tiles(g), narrow = q8_few_shape(g).nt == 1;
+    int splits = 1;
+    bool few = true;
+    for (int n = 2; n <= 16; n *= 2) {
+        const double join = time_of_join(g, n);
+        if (narrow && g.K >= 1024 * n && time_of_few(g, n) + join < time) {
+            time = time_of_few(g, n) + join;
+            splits = n;
+            few = true;
+        }
+        if (fits && g.K >= 512 * n && time_of_tiles(g, n) + join < time) {
+            time = time_of_tiles(g, n) + join;
+            splits = n;
+            few = false;
+        }
+    }
+    if (splits == 1) return EMU_OK;
+    const int64_t ld = up(g.N, 4), bytes = splits * g.R * ld * 4;
+    if (bytes > MOST_COPIED) return EMU_OK;
+    char *at = nullptr;
+    if (int rc = api_try_workspace(bytes, &at)) return rc;
+    if (!at) return EMU_OK;
+    *done = true;
+    Q8Gemm d = g;
+    d.Y = at;
+    d.ldy = ld;
+    d.part = (int)up((g.K + splits - 1) / splits, 128);
+    const int n = (g.K + d.part - 1) / d.part;
+    hipError_t e = few ? launch_q8_few_sums(d, n, s) : launch_q8_tiles_sums(d, n, s);
+    if (e == hipSuccess)
+        with_type(g.dtype, [&](auto z) {
+            q8_join_kernel<decltype(z)><<<(unsigned)((g.R * (ld / 4) + 255) / 256), 256, 0, s>>>(
+                g, reinterpret_cast<const int *>(at), ld, n);
+        });
+    return api_done(e == hipSuccess ? hipGetLastError() : e, "q8_gemm");
+}
+
+// The product on copies of the operands that the kernel of q8_tiles.h cannot take: d, with the
+// copies to be made (to workspace that d does not have yet).
+struct OnCopies {
+    Copied x, w;
+    Q8Gemm d;
+    bool possible;
+    int64_t xb() const { return up(x.bytes(), 256); }
+    int64_t bytes() const { return xb() + w.bytes(); }
+    double time() const { return 8 + bytes() * 2 / 4e6 + time_of_tiles(d); }
+};
+static OnCopies on_copies(const Q8Gemm &g) {
+    OnCopies c = {};
     // the rows of X through their numbers into the copy, where those are fewer
     const int *const map = g.rows && g.xrows > g.R ? g.rows : nullptr;
     const int64_t K = up(g.K, 16), xr = g.rows && !map ? g.xrows : g.R;
     const bool pad = K != g.K, x = pad || !aligned16(g.X) || g.ldx % 16 || (map && g.xrows * g.ldx >= OFFSETS);
     const bool w = pad || !aligned16(g.W) || g.ldw % 16 || g.sw % 16;
     const int mats = g.sw == 0 ? 1 : g.E;                       // one matrix for all experts
-    const Copied cx = {g.X, g.ldx, 0, g.xrows, g.K, map, x ? 1 : 0, nullptr, 0, xr, K};
-    const Copied cw = {g.W, g.ldw, g.sw, g.N, g.K, nullptr, w ? mats : 0, g.sw == 0 ? nullptr : g.offsets, g.R, g.N, K};
-    const int64_t xb = up(cx.bytes(), 256), wb = cw.bytes();
-    Q8Gemm d = g;
-    d.K = (int)K;
+    c.x = {g.X, g.ldx, 0, g.xrows, g.K, map, x ? 1 : 0, nullptr, 0, xr, K};
+    c.w = {g.W, g.ldw, g.sw, g.N, g.K, nullptr, w ? mats : 0, g.sw == 0 ? nullptr : g.offsets, g.R, g.N, K};
+    c.d = g;
+    c.d.K = (int)K;
     if (x) {
-        d.X = nullptr;
-        d.ldx = K;
-        if (map) d.rows = nullptr;
+        c.d.X = nullptr;
+        c.d.ldx = K;
+        if (map) c.d.rows = nullptr;
     }
     if (w) {
-        d.W = nullptr;
-        d.ldw = K;
-        d.sw = g.sw == 0 ? 0 : cw.rows * K;
+        c.d.W = nullptr;
+        c.d.ldw = K;
+        c.d.sw = g.sw == 0 ? 0 : c.w.rows * K;
     }
+    c.possible = fits_tiles(c.d) && c.bytes() <= MOST_COPIED;
+    return c;
+}
+
+int launch_q8_gemm(const Q8Gemm &g, hipStream_t s) {
+    // the sums of rows without entries, or without any row to read, are zeros
+    if (g.K == 0 || g.E == 0 || g.xrows == 0) return api_done(launch_q8_few(g, s), "q8_gemm");
+    const bool fits = fits_tiles(g);
+    OnCopies c = {};
+    if (!fits) c = on_copies(g);
+    const double few = time_of_few(g), tiles = fits ? time_of_tiles(g) : (c.possible ? c.time() : few);
+    bool done;
+    if (int rc = split_gemm(g, few < tiles ? few : tiles, s, &done)) return rc;
+    if (done) return EMU_OK;
+    if (fits && tiles < few) return api_done(run_tiles_kernel(g, s), "q8_gemm");
     char *at = nullptr;
-    if (fits_tiles(d) && xb + wb <= MOST_COPIED && 8 + (xb + wb) * 2 / 4e6 + tiles < few)
-        if (int rc = api_try_workspace(xb + wb, &at)) return rc;
+    if (!fits && tiles < few)
+        if (int rc = api_try_workspace(c.bytes(), &at)) return rc;
     if (!at) return api_done(launch_q8_few(g, s), "q8_gemm");
-    if (x) d.X = reinterpret_cast<int8_t *>(at);
-    if (w) d.W = reinterpret_cast<int8_t *>(at + xb);
-    hipError_t e = copy(cx, at, cw, at + xb, s);
-    if (e == hipSuccess) e = run_tiles_kernel(d, s);
+    if (c.x.mats > 0) c.d.X = reinterpret_cast<int8_t *>(at);
+    if (c.w.mats > 0) c.d.W = reinterpret_cast<int8_t *>(at + c.xb());
+    hipError_t e = copy(c.x, at, c.w, at + c.xb(), s);
+    if (e == hipSuccess) e = run_tiles_kernel(c.d, s);
     return api_done(e, "q8_gemm");
 }
 

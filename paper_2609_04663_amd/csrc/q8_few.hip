@@ -13,7 +13,7 @@
 namespace emu {
 namespace {
 
-constexpr int STEP = 128, WAVES = 8, THREADS = 64 * WAVES;
+constexpr int STEP = 128, WAVES = Q8_FEW_ROUND / STEP, THREADS = 64 * WAVES;
 
 __device__ __forceinline__ i32x4 mfma16(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
@@ -102,17 +102,23 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
         int sum = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) sum += share[w][r / 16][c / 16][r % 16 * 16 + c % 16];
-        const int64_t at = g.rows ? g.rows[t.first + r] : t.first + r;
-        const bool there = at >= 0 && at < g.xrows;   // zeros for a row outside X, whatever W's scale
-        const double y = there ? (double)sum * g.ws[(int64_t)t.e * N + col0 + c] * g.xs[at] : 0.0;
-        Y[r * g.ldy + c] = (T)(float)y;
+        if constexpr (std::is_same<T, int>::value) {
+            Y[r * g.ldy + c] = sum;
+        } else {
+            const int64_t at = g.rows ? g.rows[t.first + r] : t.first + r;
+            const bool there = at >= 0 && at < g.xrows;   // zeros for a row outside X, whatever W's scale
+            const double y = there ? (double)sum * g.ws[(int64_t)t.e * N + col0 + c] * g.xs[at] : 0.0;
+            Y[r * g.ldy + c] = (T)(float)y;
+        }
     }
 }
 
+// T int: the sums of a split.
 template <typename T, int MT, int NT>
 __global__ __launch_bounds__(THREADS, MT + NT >= 6 ? 2 : 4) void q8_few_kernel(Q8Gemm g) {
     constexpr int COLS = 16 * NT;
     __shared__ int share[WAVES][MT][NT][256];
+    if constexpr (std::is_same<T, int>::value) to_split(g);
     const RowTiles tiles(g.offsets, g.E, g.R, 16 * MT, (g.N + COLS - 1) / COLS);
     for (int64_t id = blockIdx.x;; id += gridDim.x) {
         const RowTile t = tiles.at(id);
@@ -138,32 +144,43 @@ static int column_sets(const Q8Gemm &g) {
     return expected(g, 4) >= cus ? 4 : (expected(g, 2) >= cus ? 2 : 1);
 }
 
-double q8_few_traffic(const Q8Gemm &g) {
+Q8FewShape q8_few_shape(const Q8Gemm &g) {
     const int mt = row_sets(g), nt = column_sets(g);
-    return (double)expected(g, nt) * g.K * 16 * (mt + nt);
+    return {(double)expected(g, nt), mt, nt};
 }
 
-hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s) {
+template <typename T>
+static void launch(const Q8Gemm &g, int splits, hipStream_t s) {
     using std::integral_constant;
     // (no expert: rows of zeros)
     const int mt = g.E > 0 ? row_sets(g) : 4, nt = g.E > 0 ? column_sets(g) : 4;
     auto tiles = [&](int nt) { return row_blocks_bound(g.R, g.E, 16 * mt) * ((g.N + 16 * nt - 1) / (16 * nt)); };
-    with_type(g.dtype, [&](auto z) {
-        using T = decltype(z);
-        auto run = [&](auto m, auto n) {
-            constexpr int MT = decltype(m)::value, NT = decltype(n)::value;
-            constexpr int64_t MOST = 1 << 22;
-            q8_few_kernel<T, MT, NT><<<(unsigned)(tiles(NT) < MOST ? tiles(NT) : MOST), THREADS, 0, s>>>(g);
-        };
-        auto columns = [&](auto m) {
+    auto run = [&](auto m, auto n) {
+        constexpr int MT = decltype(m)::value, NT = decltype(n)::value;
+        const int64_t most = (1 << 22) / splits;
+        const dim3 grid((unsigned)(tiles(NT) < most ? tiles(NT) : most), splits);
+        q8_few_kernel<T, MT, NT><<<grid, THREADS, 0, s>>>(g);
+    };
+    auto columns = [&](auto m) {
+        if constexpr (std::is_same<T, int>::value) {
+            run(m, integral_constant<int, 1>{});        // splits are of few columns
+        } else {
             if (nt == 1) run(m, integral_constant<int, 1>{});
             else if (nt == 2) run(m, integral_constant<int, 2>{});
             else run(m, integral_constant<int, 4>{});
-        };
-        if (mt == 1) columns(integral_constant<int, 1>{});
-        else if (mt == 2) columns(integral_constant<int, 2>{});
-        else columns(integral_constant<int, 4>{});
-    });
+        }
+    };
+    if (mt == 1) columns(integral_constant<int, 1>{});
+    else if (mt == 2) columns(integral_constant<int, 2>{});
+    else columns(integral_constant<int, 4>{});
+}
+
+hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s) {
+    with_type(g.dtype, [&](auto z) { launch<decltype(z)>(g, 1, s); });
+    return hipGetLastError();
+}
+hipError_t launch_q8_few_sums(const Q8Gemm &g, int splits, hipStream_t s) {
+    launch<int>(g, splits, s);
     return hipGetLastError();
 }
 

@@ -57,6 +57,8 @@ template <typename T, int RB, int STAGES, bool GATHER>
 struct Q8Source {
     static constexpr int TILE = 64 * RB;
     static constexpr bool DRAINED = true;
+    static constexpr bool SUMS = std::is_same<T, int>::value;   // 32-bit sums without scales
+    using Out = std::conditional_t<SUMS, float, T>;             // their bits
     using A = ByteSide<RB>;
     using B = ByteSide<RB>;
     static_assert(A::COPIES % 2 == 0, "a wave's copies start at an even one");
@@ -127,7 +129,7 @@ struct Q8Source {
     // in flight too (loads return in order).  No copy is when a tile starts.
     __device__ __forceinline__ void open() {
         turn ^= 1;
-        if (wave * 64 < TILE) {
+        if (!SUMS && wave * 64 < TILE) {
             Scales<TILE> &s = scales[turn];
             const int64_t n = (int64_t)now.col * TILE + threadIdx.x;
             const bool there = row >= 0 && row < g.xrows;
@@ -176,6 +178,11 @@ struct Q8Source {
         // sum out of the range of normal numbers
         const Scales<TILE> &s = scales[turn];
         const int rows = (int)(now.end - now.first), cols = g.N - now.col * TILE;
+        if (SUMS) {
+            if (cols >= TILE) store_rows<true>(acc, s, rows, cols);
+            else store_rows<false>(acc, s, rows, cols);
+            return;
+        }
         bool special = cols < TILE;
 #pragma unroll
         for (int i = lane; i < RB * 32; i += 64) {
@@ -191,14 +198,14 @@ struct Q8Source {
                                                int cols) const {
         typedef float f32x4 __attribute__((ext_vector_type(4)));
         const int l = lane_here(), h = l >> 5, col0 = (wave & 1) * RB * 32;
-        T *const Y = static_cast<T *>(g.Y) + now.first * g.ldy + now.col * TILE + col0;
+        Out *const Y = static_cast<Out *>(g.Y) + now.first * g.ldy + now.col * TILE + col0;
 #pragma unroll
         for (int i = 0; i < RB; ++i) {
             const int row = ((wave >> 1) * RB + i) * 32 + (l & 31);
             if (row >= rows) continue;
-            T *const p = Y + row * g.ldy + (sizeof(T) == 4 ? 4 : 8) * h;
-            const float x = s.x[row];
-            const bool keep = PLAIN || s.there[row];   // zeros for a row outside X, whatever W's scale
+            Out *const p = Y + row * g.ldy + (sizeof(T) == 4 ? 4 : 8) * h;
+            const float x = SUMS ? 1.0f : s.x[row];
+            const bool keep = PLAIN || SUMS || s.there[row];    // zeros for a row outside X, whatever W's scale
 #pragma unroll
             for (int j = 0; j < RB; ++j) {
                 __builtin_amdgcn_sched_barrier(0);          // few values in flight: no registers to spare
@@ -211,7 +218,9 @@ struct Q8Source {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
                         const float sum = (float)acc[i][j][r + k], m = w[k / 4][k % 4];
-                        if constexpr (PLAIN)
+                        if constexpr (SUMS)
+                            y[k] = __int_as_float(acc[i][j][r + k]);
+                        else if constexpr (PLAIN)
                             y[k] = sum * m * x;
                         else
                             y[k] = ldexpf(sum * __builtin_amdgcn_frexp_mantf(m) * __builtin_amdgcn_frexp_mantf(x),
@@ -224,7 +233,7 @@ struct Q8Source {
     }
     // y: columns 4 h .. 4 h + 3 and 8 + 4 h .. of 16, of which `cols` exist; p: the lane's first
     template <bool PLAIN>
-    __device__ __forceinline__ void store8(T *p, bool keep, int cols, float (&y)[8]) const {
+    __device__ __forceinline__ void store8(Out *p, bool keep, int cols, float (&y)[8]) const {
         if constexpr (sizeof(T) == 4) {
             const int first = 4 * (lane >> 5);
 #pragma unroll
@@ -265,6 +274,7 @@ struct Q8Source {
     }
 };
 
+// T int: the sums of a split.
 template <typename T, int RB, int STAGES, bool GATHER>
 __global__ __launch_bounds__(256, RB * STAGES == 4 ? 2 : 1) void q8_tiles_kernel(Q8Gemm g) {
     using Source = Q8Source<T, RB, STAGES, GATHER>;
@@ -272,6 +282,7 @@ __global__ __launch_bounds__(256, RB * STAGES == 4 ? 2 : 1) void q8_tiles_kernel
     __shared__ TileList list;
     __shared__ __attribute__((aligned(16))) Scales<Source::TILE> scales[2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (Source::SUMS) to_split(g);
     list.fill(g, Source::TILE);
     Source src(g, list, scales, wave, lane);
     if (src.start()) run_tiles<i8pair, RB, STAGES, RB == 2 ? 2 : 1>(src, lds, wave);

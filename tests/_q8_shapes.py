@@ -13,3 +13,6 @@ SHAPES = [(17, 1, 128, 16), (130, 1, 130, 48), (200, 2, 257, 112), (300, 3, 100,
 ODD = [(100, 1, 130, 1), (300, 3, 257, 77), (1000, 5, 129, 1001), (2500, 2, 700, 333), (5000, 4, 700, 333), (4000, 2, 1000, 1001)]
 # more tiles than workgroups
 LARGE = [(33000, 3, 1030, 144), (20000, 70, 2048, 128), (16000, 1, 4100, 400)]
+# long reductions of few tiles, in splits
+SPLIT = [(3, 1, 40, 30001), (20, 1, 30, 21600), (39, 1, 64, 6656), (50, 1, 33, 40007), (294, 1, 300, 8128),
+         (130, 1, 260, 20016)]

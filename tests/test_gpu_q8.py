@@ -151,7 +151,7 @@ def _check(emu, X, xs, W, ws, offsets, rows, dt, X_=None, W_=None):
 
 @pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("kind", list(M.TYPES))
-@pytest.mark.parametrize("R,E,N,K", S.FEW + S.SHAPES + S.ODD)
+@pytest.mark.parametrize("R,E,N,K", S.FEW + S.SHAPES + S.ODD + S.SPLIT)
 def test_product(emu, kind, R, E, N, K, gather):
     _check(emu, *_operands(R + N + K, R, E, N, K, gather), M.TYPES[kind])
 
@@ -308,6 +308,24 @@ def test_few_of_many_rows_through_a_copy(emu, K, lead):
     rows = torch.randint(-5, T + 5, (R,), generator=gen).int()
     offsets = torch.tensor([0, 1700, 2900], dtype=torch.int32)
     _check(emu, X, xs, W, ws, offsets, rows, torch.float32, whole.cuda()[lead:].view(T, K))
+
+
+@pytest.mark.parametrize("R", [50, 294])
+def test_split_of_some_rows(emu, R):
+    """Offsets that leave rows without an expert, an output of its own type and leading
+    dimension, scales that are not finite."""
+    X, xs, W, ws, _, rows = _operands(R, R, 1, 130, 8128, True)
+    offsets = torch.tensor([0, R - 7], dtype=torch.int32)
+    ref = Q.product(X, xs, W, ws, offsets, rows)
+    whole = torch.full((R + 1, 140), 5.0, dtype=torch.float16).cuda()
+    ws[0, 3] = math.nan
+    emu.q8_gemm(X.cuda(), xs.cuda(), W.cuda(), ws.cuda(), offsets.cuda(), rows.cuda(), Y=whole[:R, 5:135])
+    got = whole[:R, 5:135].clone()
+    outside = (rows < 0) | (rows >= X.shape[0]) | (torch.arange(R) >= R - 7)
+    assert torch.isnan(got[~outside.cuda(), 3]).all() and (got[outside.cuda()] == 0).all()
+    got[:, 3], ref[:, 3] = 0, 0
+    M.check(got, ref, Q.product_bar(ref, torch.float16))
+    assert (whole[:, :5] == 5).all() and (whole[:, 135:] == 5).all() and (whole[R] == 5).all()
 
 
 def test_many_odd_rows_without_workspace(emu):

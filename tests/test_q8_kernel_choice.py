@@ -49,6 +49,9 @@ for _ in range(20000):
     N, K = (int(2 ** rng.uniform(0, 13.5)) for _ in range(2))
     K = K if rng.random() < 0.3 else K // 16 * 16 + 16
     seen.update(gemm(rng.randrange(3), R, E, N, K, rng.random() < 0.5, rng.choice([None, 2 * R])))
+for _ in range(3000):
+    R, N, K = (int(2 ** rng.uniform(a, b)) for a, b in ((0, 11), (0, 12), (11, 16)))
+    seen.update(gemm(rng.randrange(3), R, 1, N, K // 16 * 16, rng.random() < 0.5))
 result = [sorted(seen), L.all_kernels()]
 """)
     ours = [k for k in held if k.startswith(("balance_", "q8_"))]
@@ -57,15 +60,18 @@ result = [sorted(seen), L.all_kernels()]
 
 def test_shapes_of_the_gpu_tests(fake):
     """Each group reaches its kernels; together all of them."""
-    few, tiles, odd, large = F.run(fake, CALLS + """
+    few, tiles, odd, large, splits = F.run(fake, CALLS + """
 result = [[[k for gather in (False, True) for k in gemm(1, *s, gather)] for s in g]
-          for g in (S.FEW, S.SHAPES, S.ODD, S.LARGE)]
+          for g in (S.FEW, S.SHAPES, S.ODD, S.LARGE, S.SPLIT)]
 """)
     reached = {k for ks in few for k in ks if k.startswith("q8_few_kernel<bf16")}
     assert len(reached) == 9, reached
     reached = {k for ks in few + tiles + odd + large for k in ks if k.startswith("q8_tiles_kernel<bf16")}
     assert len(reached) == 6, reached
     assert sum("q8_copy_kernel" in ks for ks in odd) >= 2
+    assert {k for ks in splits for k in ks} >= {
+        "q8_few_kernel<int, 1, 1>", "q8_few_kernel<int, 2, 1>", "q8_few_kernel<int, 4, 1>",
+        "q8_tiles_kernel<int, 2, 4, false>", "q8_tiles_kernel<int, 2, 4, true>", "q8_join_kernel<bf16>"}
     assert all(any(k.startswith("q8_tiles_kernel") for k in ks) for ks in large)
 
 
@@ -77,12 +83,14 @@ result = [gemm(1, 4000, 1, 1000, 1001), gemm(1, 4000, 1, 1000, 1024, x=F.X + 1),
 assert L.emu.emu_release_workspace() == 0
 L.fake.fake_room(0)
 result += [gemm(1, 4000, 1, 1000, 1001), gemm(1, 4000, 1, 1000, 1024), L.emu.emu_workspace_bytes()]
+result.append([gemm(1, *s) for s in S.SPLIT])
 """)
     for kernels in got[:2]:
         assert kernels[0] == "q8_copy_kernel" and kernels[1].startswith("q8_tiles_kernel") and len(kernels) == 2
     assert got[2] and got[5] == 0
     assert len(got[3]) == 1 and got[3][0].startswith("q8_few_kernel")
     assert len(got[4]) == 1 and got[4][0].startswith("q8_tiles_kernel")
+    assert all(len(kernels) == 1 for kernels in got[6])
 
 
 def test_copies_take_the_fewer_rows(fake):
