@@ -83,12 +83,12 @@ bool fits_tiles(const Q8Gemm &g) {
 // 8 rows 10 and 16, 32 rows 25 and 19, 128 rows 47 and 38, 4096 rows 144 and 50; 13 of 1501 x 777,
 // 100 rows 15 and 24 (with the copies).
 int64_t tiles_of(const Q8Gemm &g, int64_t t) { return row_blocks_expected(g.R, g.E, t) * ((g.N + t - 1) / t); }
-// The kernel for few rows: its waves read X and W at 7 to 8 TB/s, at half of it from rows that
-// are not multiples of 16 bytes, the matrices come at 6 TB/s; a workgroup takes 1024 indices
+// The kernel for few rows: its waves read X and W at 7 to 8 TB/s, the matrices come at 6 TB/s,
+// both at a third of it from rows that are not multiples of 16 bytes; a workgroup takes 1024 indices
 // in 0.7 to 2.5 us, by its loads; the largest tiles are alone on a CU and take 6 us beside.
 double time_of_few(const Q8Gemm &g, int splits = 1) {
     const Q8FewShape f = q8_few_shape(g);
-    const double cus = (double)device_cu_count(), loads = f.mt + f.nt, aligned = g.K % 16 == 0 ? 1 : 0.5;
+    const double cus = (double)device_cu_count(), loads = f.mt + f.nt, aligned = g.K % 16 == 0 ? 1 : 0.33;
     const double rounds = (double)(up(g.K, Q8_FEW_ROUND * splits) / (Q8_FEW_ROUND * splits));
     double t = (0.1 + 0.3 * loads) * rounds * ceil(f.tiles * splits / (2 * cus));
     t = fmax(t, f.tiles * g.K * 16 * loads / ((g.E > 1 ? 7e6 : 8e6) * aligned));

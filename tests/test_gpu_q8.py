@@ -330,7 +330,7 @@ def test_split_of_some_rows(emu, R):
 
 def test_many_odd_rows_without_workspace(emu):
     """A captured call that finds no workspace reads the operands as they are."""
-    X, xs, W, ws, offsets, rows = _operands(3, 2500, 3, 300, 515, True)
+    X, xs, W, ws, offsets, rows = _operands(3, 2500, 3, 600, 515, True)
     ref = Q.product(X, xs, W, ws, offsets, rows)
     args = [t.cuda() for t in (X, xs, W, ws, offsets, rows)]
     eager = emu.q8_gemm(*args)
