@@ -251,8 +251,6 @@ struct RowSide : StridedSide<RB> {
 //   src.copied()     the copies of a k-block have been started
 //   src.blocks()     k-blocks of the current tile, at least STAGES
 //   src.close(acc)   the tile is done; false: it was the last
-//   Source::DRAINED  close() waits for every copy before it stores, so that the next tile's
-//                    first trip need not: its stores have two trips to end in
 //   LEAD             sub-steps that fragments are read ahead; with 2 the stage is given back a
 //                    sub-step earlier
 template <typename T, int RB, int STAGES = 2, int LEAD = 1, typename Source>
@@ -279,7 +277,7 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
         static_for<COPIES>([&](auto c) { copy(c, lds + i * STAGE); });
         src.copied();
     }
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - (Source::DRAINED ? 2 : 1)) * COPIES) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * COPIES) : "memory");
     __syncthreads();
     src.arrived(lds, 0);
     static_for<LEAD>([&](auto s) { static_for<2 * RB>([&](auto u) { read(f[s], lds, s, u); }); });
@@ -313,9 +311,8 @@ __device__ __forceinline__ void run_tiles(Source &src, char *lds, int wave) {
             src.trip();
             static_for<SUBS - LEAD>([&](auto i) { step(i, cur, std::false_type{}); });
             __builtin_amdgcn_sched_barrier(0);
-            if (Source::DRAINED && decltype(first)::value)
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            else if (STAGES == 2)
+            // (copies land in order; stores in flight can only make the wait longer)
+            if (STAGES == 2)
                 asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             else
                 asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * COPIES) : "memory");
@@ -430,7 +427,6 @@ struct TileList {
 template <typename T, int RB, bool TB, bool GATHER>
 struct GemmSource {
     static constexpr int TILE = 64 * RB;
-    static constexpr bool DRAINED = false;
     using A = Side<RB, CONTIG>;
     using B = Side<RB, TB ? CONTIG : STRIDED>;
     const GroupedGemm &g;
@@ -539,7 +535,6 @@ __global__ __launch_bounds__(256, RB == 4 ? 1 : 2) void gemm16_kernel(GroupedGem
 template <typename T, int RB, int MAPPED>        // the operand that goes through a map: 0 none, 1 P, 2 Q
 struct WgradSource {
     static constexpr int TILE = 64 * RB;
-    static constexpr bool DRAINED = false;
     static constexpr bool PIECES = RB == 2;     // an expert's rows may be in pieces (the others have no registers to spare)
     using A = RowSide<RB, MAPPED == 1>;
     using B = RowSide<RB, MAPPED == 2>;

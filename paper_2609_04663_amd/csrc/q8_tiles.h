@@ -56,7 +56,6 @@ struct Scales {
 template <typename T, int RB, int STAGES, bool GATHER>
 struct Q8Source {
     static constexpr int TILE = 64 * RB;
-    static constexpr bool DRAINED = true;
     static constexpr bool SUMS = std::is_same<T, int>::value;   // 32-bit sums without scales
     using Out = std::conditional_t<SUMS, float, T>;             // their bits
     using A = ByteSide<RB>;
@@ -126,7 +125,7 @@ struct Q8Source {
         return true;
     }
     // The scales go straight to LDS: waiting for them in registers would wait for the copies
-    // in flight too (loads return in order).  No copy is when a tile starts.
+    // in flight too (loads return in order).
     __device__ __forceinline__ void open() {
         turn ^= 1;
         if (!SUMS && wave * 64 < TILE) {
@@ -172,8 +171,7 @@ struct Q8Source {
     // block.  16-bit results are exchanged between the lane halves: eight neighbouring
     // columns of a row to a lane, one 16-byte store.
     __device__ __forceinline__ void store(const i32x16 (&acc)[RB][RB]) const {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        pipeline_barrier();                                 // the scales of every wave
+        // (the scales have landed: a barrier of the second or, of four stages, the third trip)
         // whether a row does not exist in X, or a column's scale could take its product with a
         // sum out of the range of normal numbers
         const Scales<TILE> &s = scales[turn];
