@@ -81,6 +81,8 @@ def test_subnormal_rows(emu):
     q, scales = Q.pack(x)
     got, got_scales = emu.q8_pack(x.cuda())
     assert torch.equal(got.cpu(), q) and _same(got_scales, scales)
+    for dt in M.TYPES.values():
+        assert _same(emu.q8_unpack(got, got_scales, dt), (q.float() * scales[:, None]).to(dt))
 
 
 @pytest.mark.parametrize("kind", list(M.TYPES))
@@ -390,3 +392,49 @@ def test_the_run_of_them(emu):
     full = emu.moe_combine(emu.grouped_gemm(torch.nn.functional.silu(
         emu.grouped_gemm(x, W1, r.offsets, transb="T", rows=r.rows)), W2, r.offsets, transb="T"), r.slots, r.weights)
     assert float((y.float() - full.float()).norm() / full.float().norm()) < 0.05
+
+
+@pytest.mark.parametrize("kind", list(M.TYPES))
+@pytest.mark.parametrize("R,K", [(9, 100), (300, 160), (900, 1600)])
+def test_results_below_the_normal_range(emu, kind, R, K):
+    """Subnormal results of the type: off by at most half their spacing, and by the roundings
+    in FP32 before."""
+    X, xs, W, ws, _, _ = _operands(R, R, 1, 140, K, False)
+    top = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -14}[kind]
+    xs = torch.full((R,), top / 128)
+    ws = torch.full((1, 140), 1.0 / (128 * K ** 0.5 * 16))
+    ref = Q.product(X, xs, W, ws, None, None)
+    assert (ref.abs() < top).all() and (ref.abs() > top * 2.0 ** -8).any()
+    got = emu.q8_gemm(X.cuda(), xs.cuda(), W.cuda(), ws.cuda(), dtype=M.TYPES[kind])
+    # in float32 and bfloat16 the product of the scales' rounding is subnormal too
+    M.check(got, ref, Q.product_bar(ref, M.TYPES[kind]) + 2.0 ** -149)
+
+
+def test_two_graphs_and_eager_calls_share_the_workspace(emu):
+    """Graphs of a loss over many tokens, of a product on copies and of one in splits, replayed
+    in turns with eager calls between."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    logits = torch.randn((5000, 64), generator=gen, device="cuda")
+    ids = torch.topk(logits, 4).indices.int().contiguous()
+    a, sa = emu.q8_pack(torch.randn((3000, 501), generator=gen, device="cuda"))
+    b, sb = emu.q8_pack(torch.randn((700, 501), generator=gen, device="cuda"))
+    c, sc = emu.q8_pack(torch.randn((50, 30000), generator=gen, device="cuda"))
+    d, sd = emu.q8_pack(torch.randn((70, 30000), generator=gen, device="cuda"))
+    calls = [lambda: emu.moe_balance(logits, ids)[:3], lambda: (emu.q8_gemm(a, sa, b, sb),),
+             lambda: (emu.q8_gemm(c, sc, d, sd),)]
+    eager = [[t.clone() for t in f()] for f in calls]
+    graphs, out = [], []
+    for f in calls:
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out.append(f())
+        graphs.append(graph)
+    for i in (0, 1, 2, 1, 0, 2, 0):
+        for t in out[i]:
+            t.zero_()
+        graphs[i].replay()
+        again = [t.clone() for t in calls[(i + 1) % 3]()]
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(out[i], eager[i]))
+        assert all(torch.equal(u, v) for u, v in zip(again, eager[(i + 1) % 3]))
