@@ -289,6 +289,10 @@ class Routing(NamedTuple):
 
 def _float_mat(t, name: str, like=None) -> int:
     """The element code of a row-major matrix of a supported type."""
+    if type(t) is torch.Tensor and t.dim() == 2 and t.is_contiguous():      # the cheaper look
+        code = _DTYPES.get(t.dtype)
+        if code is not None and (like is None or t.dtype is like.dtype):
+            return code
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     code = _DTYPES.get(t.dtype)
@@ -625,6 +629,8 @@ def moe_balance_grad(logits, counts, tokens, dloss, dzloss=None, starts=None) ->
 
 
 def _int8_mat(t, name: str):
+    if type(t) is torch.Tensor and t.dtype is torch.int8 and t.dim() == 2 and t.is_contiguous():
+        return t
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     return _layout(t, torch.int8, name)

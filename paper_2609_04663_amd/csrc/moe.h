@@ -133,11 +133,13 @@ struct Q8Gemm {
 int launch_q8_gemm(const Q8Gemm &g, hipStream_t s);
 hipError_t launch_q8_few(const Q8Gemm &g, hipStream_t s);
 hipError_t launch_q8_few_sums(const Q8Gemm &g, int splits, hipStream_t s);
-// What its time goes by (E > 0): its tiles, their rows and columns in sixteens; indices that
-// a workgroup takes at a time.
+// What its time goes by (E > 0): its tiles, their rows and columns in sixteens, how many of
+// them share a CU, whether all rows are whole 32-bit words; indices that a workgroup takes at
+// a time.
 struct Q8FewShape {
     double tiles;
-    int mt, nt;
+    int mt, nt, per_cu;
+    bool words;
 };
 Q8FewShape q8_few_shape(const Q8Gemm &g);
 constexpr int Q8_FEW_ROUND = 1024;

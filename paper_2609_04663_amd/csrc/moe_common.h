@@ -137,7 +137,7 @@ inline int64_t row_blocks_bound(int64_t R, int64_t E, int64_t rows) {
 }
 // Experts that an even load of the rows reaches, and about so many blocks: an expert's
 // last one is half full on average.
-inline double experts_reached(int64_t R, int64_t E) { return E * (1 - pow(1 - 1.0 / E, (double)R)); }
+inline double experts_reached(int64_t R, int64_t E) { return E == 1 ? 1 : E * (1 - pow(1 - 1.0 / E, (double)R)); }
 inline int64_t row_blocks_expected(int64_t R, int64_t E, int64_t rows) {
     if (E == 1) return (R + rows - 1) / rows;
     const double reached = experts_reached(R, E), blocks = (R + reached * rows / 2) / rows;

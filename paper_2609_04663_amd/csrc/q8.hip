@@ -84,16 +84,16 @@ bool fits_tiles(const Q8Gemm &g) {
 // 100 rows 15 and 24 (with the copies).
 int64_t tiles_of(const Q8Gemm &g, int64_t t) { return row_blocks_expected(g.R, g.E, t) * ((g.N + t - 1) / t); }
 // The kernel for few rows: its waves read X and W at 7 to 8 TB/s, the matrices come at 6 TB/s,
-// both at a third of it from rows that are not multiples of 16 bytes; a workgroup takes 1024 indices
-// in 0.7 to 2.5 us, by its loads; the largest tiles are alone on a CU and take 6 us beside.
+// a workgroup takes 1024 indices in 0.7 to 2.5 us, by its loads, and 6 us beside; rows that are
+// not whole words take half as much again.
 double time_of_few(const Q8Gemm &g, int splits = 1) {
     const Q8FewShape f = q8_few_shape(g);
-    const double cus = (double)device_cu_count(), loads = f.mt + f.nt, aligned = g.K % 16 == 0 ? 1 : 0.33;
+    const double cus = (double)device_cu_count(), loads = f.mt + f.nt, more = f.words ? 1 : 1.5;
     const double rounds = (double)(up(g.K, Q8_FEW_ROUND * splits) / (Q8_FEW_ROUND * splits));
-    double t = (0.1 + 0.3 * loads) * rounds * ceil(f.tiles * splits / (2 * cus));
-    t = fmax(t, f.tiles * g.K * 16 * loads / ((g.E > 1 ? 7e6 : 8e6) * aligned));
-    t = fmax(t, experts_reached(g.R, g.E) * g.N * g.K / (6e6 * aligned));
-    return (g.E > 1 ? 8 : 5) + t + (loads == 8 ? f.tiles * splits / cus * 6 : 0);
+    double t = ceil(f.tiles * splits / (f.per_cu * cus)) * (6 + (0.1 + 0.3 * loads) * rounds * more) - 6;
+    t = fmax(t, f.tiles * g.K * 16 * loads * more / (g.E > 1 ? 7e6 : 8e6));
+    t = fmax(t, experts_reached(g.R, g.E) * g.N * g.K * more / 6e6);
+    return (g.E > 1 ? 8 : 5) + t;
 }
 // Tiles of 128 take 0.45 us for a k-block (copies to LDS at 64 bytes a cycle and the reads of
 // fragments), all of them the matrices' bytes at 6 TB/s.
@@ -155,7 +155,7 @@ hipError_t run_tiles_kernel(const Q8Gemm &g, hipStream_t s) {
 // 49; 39 of 64 x 6656 16 and, in four, 11; 16 of 2048 x 16384 17 and, in 16, 23.
 static int split_gemm(const Q8Gemm &g, double time, hipStream_t s, bool *done) {
     *done = false;
-    if (g.E != 1) return EMU_OK;
+    if (g.E != 1 || g.K < 1024) return EMU_OK;
     const bool fits = fits_tiles(g), narrow = q8_few_shape(g).nt == 1;
     int splits = 1;
     bool few = true;
@@ -201,7 +201,7 @@ struct OnCopies {
     bool possible;
     int64_t xb() const { return up(x.bytes(), 256); }
     int64_t bytes() const { return xb() + w.bytes(); }
-    double time() const { return 8 + bytes() * 2 / 4e6 + time_of_tiles(d); }
+    double time() const { return 4 + bytes() * 2 / 6e6 + time_of_tiles(d); }
 };
 static OnCopies on_copies(const Q8Gemm &g) {
     OnCopies c = {};

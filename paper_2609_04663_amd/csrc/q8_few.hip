@@ -23,24 +23,56 @@ __device__ __forceinline__ i32x4 mfma16(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
-template <int N>
+// The N rows of a lane.  SHIFT: not all of them at multiples of 4, where a 16-byte load of
+// its own address takes two to three times as long: five whole words around the bytes are
+// read, and moved when they are used.  Not in a matrix's first and last rows, whose
+// words may lie partly outside of it.  16 rows of 16384 x 8192 at odd addresses: 34 us, with
+// the loads of their own addresses 73; 60 of 4096 x 4095 20 and 31.
+template <int N, bool SHIFT>
+struct Rows {
+    const int8_t *at[N];
+    int by[N];                      // bytes that at[i] lies before the row
+    __device__ __forceinline__ void set(int i, const int8_t *row, bool edge) {
+        by[i] = SHIFT && !edge ? (int)((uintptr_t)row & 3) : 0;
+        at[i] = row - by[i];
+    }
+};
+template <int N, bool SHIFT>
 struct Piece {                      // 128 indices of N rows of a lane
     i32x4 v[N][2];
-    __device__ __forceinline__ void load(const int8_t *const (&row)[N], int k0, int K, int h) {
+    int last[SHIFT ? N : 1][2];
+    __device__ __forceinline__ void load(const Rows<N, SHIFT> &row, int k0, int K, int h) {
         typedef int __attribute__((ext_vector_type(4), aligned(1))) unaligned;
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 const int k = k0 + 64 * p + 16 * h;
-                if (k0 + STEP <= K) v[i][p] = *reinterpret_cast<const unaligned *>(row[i] + k);
-                else v[i][p] = load_bytes16(row[i], k, K);
+                if (k0 + STEP <= K) {
+                    v[i][p] = *reinterpret_cast<const unaligned *>(row.at[i] + k);
+                    if constexpr (SHIFT)
+                        last[i][p] = row.by[i] > 0 ? *reinterpret_cast<const int *>(row.at[i] + k + 16) : 0;
+                } else {
+                    v[i][p] = load_bytes16(row.at[i] + row.by[i], k, K);
+                }
             }
+    }
+    // whole: of a step that the row does not end in
+    __device__ __forceinline__ i32x4 get(const Rows<N, SHIFT> &row, int i, int p, bool whole) const {
+        if constexpr (!SHIFT) return v[i][p];
+        const int by = whole ? row.by[i] : 0;
+        i32x4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int next = j < 3 ? v[i][p][(j + 1) % 4] : last[SHIFT ? i : 0][p];
+            r[j] = (int)__builtin_amdgcn_alignbyte((unsigned)next, (unsigned)v[i][p][j], by);
+        }
+        return r;
     }
 };
 
 // One tile; share: the waves' sums.
-template <typename T, int MT, int NT>
+template <typename T, int MT, int NT, bool SHIFT>
 __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, int (&share)[WAVES][MT][NT][256]) {
     constexpr int COLS = 16 * NT;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 4;
@@ -52,22 +84,24 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
         return;
     }
     const int steps = (K + STEP - 1) / STEP, rounds = (steps + WAVES - 1) / WAVES;
-    const int8_t *xrow[MT], *wrow[NT];
+    Rows<MT, SHIFT> xrow;
+    Rows<NT, SHIFT> wrow;
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        const int n = col0 + 16 * i + (lane & 15);
-        wrow[i] = g.W + t.e * g.sw + (int64_t)(n < N ? n : N - 1) * g.ldw;
+        const int col = col0 + 16 * i + (lane & 15), n = col < N ? col : N - 1;
+        wrow.set(i, g.W + t.e * g.sw + n * g.ldw, n == 0 || n == N - 1);
     }
 #pragma unroll
     for (int a = 0; a < MT; ++a) {                    // rows past the last repeat it, ones outside X row 0
         const int r = 16 * a + (lane & 15);
         int64_t at = t.first + (r < m ? r : m - 1);
         if (g.rows) at = g.rows[at];
-        xrow[a] = g.X + (at >= 0 && at < g.xrows ? at : 0) * g.ldx;
+        at = at >= 0 && at < g.xrows ? at : 0;
+        xrow.set(a, g.X + at * g.ldx, at == 0 || at == g.xrows - 1);
     }
     i32x4 acc[MT][NT] = {};
-    Piece<NT> w, w_next;
-    Piece<MT> x, x_next;
+    Piece<NT, SHIFT> w, w_next;
+    Piece<MT, SHIFT> x, x_next;
     auto k_of = [&](int round) {
         const int s = round * WAVES + wave;
         return (s < steps ? s : steps - 1) * STEP;    // past the end: the last ones, not used
@@ -85,12 +119,19 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
             x_next.load(xrow, k_of(round + 1), K, h);
         }
         if (round * WAVES + wave < steps) {
+            const bool whole = k_of(round) + STEP <= K;
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
+            for (int p = 0; p < 2; ++p) {
+                i32x4 f[MT];
 #pragma unroll
-                for (int i = 0; i < NT; ++i)
+                for (int a = 0; a < MT; ++a) f[a] = x.get(xrow, a, p, whole);
 #pragma unroll
-                    for (int a = 0; a < MT; ++a) acc[a][i] = mfma16(x.v[a][p], w.v[i][p], acc[a][i]);
+                for (int i = 0; i < NT; ++i) {
+                    const i32x4 c = w.get(wrow, i, p, whole);
+#pragma unroll
+                    for (int a = 0; a < MT; ++a) acc[a][i] = mfma16(f[a], c, acc[a][i]);
+                }
+            }
         }
     }
 #pragma unroll
@@ -117,9 +158,12 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
     }
 }
 
+// Workgroups to a CU, by the registers that the kernel needs.
+constexpr int few_per_cu(int mt, int nt, bool shift) { return mt + nt >= (shift ? 4 : 6) ? 1 : 2; }
+
 // T int: the sums of a split.
-template <typename T, int MT, int NT>
-__global__ __launch_bounds__(THREADS, MT + NT >= 6 ? 2 : 4) void q8_few_kernel(Q8Gemm g) {
+template <typename T, int MT, int NT, bool SHIFT>
+__global__ __launch_bounds__(THREADS, 2 * few_per_cu(MT, NT, SHIFT)) void q8_few_kernel(Q8Gemm g) {
     constexpr int COLS = 16 * NT;
     __shared__ int share[WAVES][MT][NT][256];
     if constexpr (std::is_same<T, int>::value) to_split(g);
@@ -127,7 +171,7 @@ __global__ __launch_bounds__(THREADS, MT + NT >= 6 ? 2 : 4) void q8_few_kernel(Q
     for (int64_t id = blockIdx.x;; id += gridDim.x) {
         const RowTile t = tiles.at(id);
         if (t.e < 0) return;
-        q8_few_tile<T, MT, NT>(g, t, share);
+        q8_few_tile<T, MT, NT, SHIFT>(g, t, share);
         __syncthreads();                              // every sum has been read
     }
 }
@@ -143,14 +187,19 @@ static int row_sets(const Q8Gemm &g) {
 static int64_t expected(const Q8Gemm &g, int nt) {
     return row_blocks_expected(g.R, g.E, 16 * row_sets(g)) * ((g.N + 16 * nt - 1) / (16 * nt));
 }
+static bool in_words(const Q8Gemm &g) {
+    return ((reinterpret_cast<uintptr_t>(g.X) | reinterpret_cast<uintptr_t>(g.W) | g.ldx | g.ldw | g.sw) & 3) == 0;
+}
+// (Rows that are moved take more registers: with 64 columns one workgroup has a CU; 854 rows over 64
+// experts of 1280 x 1081 73 us instead of 66.)
 static int column_sets(const Q8Gemm &g) {
     const int64_t cus = device_cu_count();
-    return expected(g, 4) >= cus ? 4 : (expected(g, 2) >= cus ? 2 : 1);
+    return expected(g, 4) >= cus && in_words(g) ? 4 : (expected(g, 2) >= cus ? 2 : 1);
 }
 
 Q8FewShape q8_few_shape(const Q8Gemm &g) {
     const int mt = row_sets(g), nt = column_sets(g);
-    return {(double)expected(g, nt), mt, nt};
+    return {(double)expected(g, nt), mt, nt, few_per_cu(mt, nt, !in_words(g)), in_words(g)};
 }
 
 template <typename T>
@@ -159,11 +208,14 @@ static void launch(const Q8Gemm &g, int splits, hipStream_t s) {
     // (no expert: rows of zeros)
     const int mt = g.E > 0 ? row_sets(g) : 4, nt = g.E > 0 ? column_sets(g) : 4;
     auto tiles = [&](int nt) { return row_blocks_bound(g.R, g.E, 16 * mt) * ((g.N + 16 * nt - 1) / (16 * nt)); };
+    const bool shift = !in_words(g);
     auto run = [&](auto m, auto n) {
         constexpr int MT = decltype(m)::value, NT = decltype(n)::value;
         const int64_t most = (1 << 22) / splits;
         const dim3 grid((unsigned)(tiles(NT) < most ? tiles(NT) : most), splits);
-        q8_few_kernel<T, MT, NT><<<grid, THREADS, 0, s>>>(g);
+        if constexpr (NT < 4)
+            if (shift) return q8_few_kernel<T, MT, NT, true><<<grid, THREADS, 0, s>>>(g);
+        q8_few_kernel<T, MT, NT, false><<<grid, THREADS, 0, s>>>(g);
     };
     auto columns = [&](auto m) {
         if constexpr (std::is_same<T, int>::value) {
