@@ -81,7 +81,7 @@ bool fits_tiles(const Q8Gemm &g) {
 // and that of tiles: 16 rows of 8192 x 8192 20 and 30; 64 rows of 4096 x 4096 14 and 18, 128 rows
 // 17 and 19; 100 rows of 8192 x 4096 22 and 18, 300 rows 57 and 21; 64 experts of 2048 x 2048,
 // 8 rows 10 and 16, 32 rows 25 and 19, 128 rows 47 and 38, 4096 rows 144 and 50; 13 of 1501 x 777,
-// 100 rows 15 and 24 (with the copies).
+// 100 rows 10 and 24 (with the copies); 64 of 1280 x 1081, 854 rows 67 and 50.
 int64_t tiles_of(const Q8Gemm &g, int64_t t) { return row_blocks_expected(g.R, g.E, t) * ((g.N + t - 1) / t); }
 // The kernel for few rows: its waves read X and W at 7 to 8 TB/s, the matrices come at 6 TB/s,
 // a workgroup takes 1024 indices in 0.7 to 2.5 us, by its loads, and 6 us beside; rows that are

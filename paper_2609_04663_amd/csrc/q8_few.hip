@@ -7,7 +7,7 @@
 // its row or column twice, 64 apart.  The waves of a workgroup take neighbouring runs of
 // 128 and add up their 32-bit sums in LDS at the end; the results are formed in FP64.
 //
-// One row of 4096 x 4096 takes 6.0 us (2.8 TB/s; a launch, and four rounds of loads that wait for
+// One row of 4096 x 4096 takes 6.2 us (2.7 TB/s; a launch, and four rounds of loads that wait for
 // one another), 8 rows over 64 experts of 2048 x 2048 9.8 with the call.  More rounds in flight
 // gained nothing (16 rows of 8192 x 8192 18.1 and, with six, 19.4 us).
 #include "emu_internal.h"
