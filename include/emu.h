@@ -357,8 +357,10 @@ int emu_q8_unpack(int dtype, int64_t rows, int64_t K, const int8_t *Q, int64_t l
      Y[r, n] = xscales[x] wscales[e, n] sum over k of X[x, k] W[e, n, k],
    e the row's expert and x its row of X, rows[r] (NULL: r itself).  dtype is Y's type.
    X: XR x K (ldx), xscales XR; W[e] starts at W + e stride and is N x K (ldw), wscales
-   E x N.  Any integers, -128 too; the sums are exact (K <= 131071).  A row of Y whose
-   row of X does not exist is zeros.  Operands whose rows are not multiples of 16 bytes are
+   E x N.  Any integers, -128 too; the sums are exact (K <= 131071), each is rounded to
+   FP32, multiplied there by wscales, then by xscales, and rounded to the type: the bits of
+   a row of Y depend on its own operands alone, not on the other rows or the workspace.  A row
+   of Y whose row of X does not exist is zeros.  Operands whose rows are not multiples of 16 bytes are
    copied to the workspace first where there are many rows; without workspace, and for
    few rows, they are read as they are. */
 int emu_q8_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, const int8_t *X, int64_t ldx,

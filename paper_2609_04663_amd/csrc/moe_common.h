@@ -191,6 +191,20 @@ __device__ __forceinline__ float exp_below(float x, float m) {
     return x == m ? 1.0f : (x > -INFINITY ? expf(x - m) : 0.0f);
 }
 
+// An 8-bit product's result from its sum and the scales of W's and X's row: three roundings in
+// FP32, the same in every kernel, so that a row's bits do not depend on which one runs.  Where
+// w could take its product with a sum (below 2^31) out of the range of normal numbers,
+// mantissas are multiplied and exponents added.
+__device__ __forceinline__ bool q8_extreme(float w) {
+    const unsigned e = __float_as_uint(w) >> 23 & 255;
+    return e > 222 || (e == 0 && w != 0.0f);        // 2^96 and more, not finite; subnormal
+}
+__device__ __forceinline__ float q8_result(int sum, float w, float x) {
+    const bool parts = q8_extreme(w);
+    const float mw = parts ? __builtin_amdgcn_frexp_mantf(w) : w, mx = parts ? __builtin_amdgcn_frexp_mantf(x) : x;
+    return ldexpf((float)sum * mw * mx, parts ? __builtin_amdgcn_frexp_expf(w) + __builtin_amdgcn_frexp_expf(x) : 0);
+}
+
 // The operands and sums of the workgroup's split (see Q8Gemm::part).
 template <typename Gemm>
 __device__ __forceinline__ void to_split(Gemm &g) {

@@ -121,11 +121,11 @@ __global__ __launch_bounds__(256) void q8_join_kernel(Q8Gemm g, const int *__res
     const bool there = r < hi && at >= 0 && at < g.xrows;
     i32x4 sum = {};
     for (int k = 0; k < splits; ++k) sum += *reinterpret_cast<const i32x4 *>(sums + (k * g.R + r) * ld + c);
-    const double x = there ? g.xs[at] : 0.0;
+    const float x = there ? g.xs[at] : 0.0f;
     T *const y = static_cast<T *>(g.Y) + r * g.ldy + c;
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (c + j < g.N) y[j] = there ? (T)(float)((double)sum[j] * g.ws[c + j] * x) : (T)0.0f;
+        if (c + j < g.N) y[j] = there ? (T)q8_result(sum[j], g.ws[c + j], x) : (T)0.0f;
 }
 
 // Times, us, of rounds of one tile of 256 on a CU, of two of 128 (or of one, where half the

@@ -5,7 +5,7 @@
 // v_mfma 16 x 16 x 64 with rows of X as rows and 16 columns of Y as columns.  A wave
 // takes 16 NT columns and 128 indices at a time: a lane loads 16 neighbouring indices of
 // its row or column twice, 64 apart.  The waves of a workgroup take neighbouring runs of
-// 128 and add up their 32-bit sums in LDS at the end; the results are formed in FP64.
+// 128 and add up their 32-bit sums in LDS at the end.
 //
 // One row of 4096 x 4096 takes 6.2 us (2.7 TB/s; a launch, and four rounds of loads that wait for
 // one another), 8 rows over 64 experts of 2048 x 2048 9.8 with the call.  More rounds in flight
@@ -152,8 +152,7 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
         } else {
             const int64_t at = g.rows ? g.rows[t.first + r] : t.first + r;
             const bool there = at >= 0 && at < g.xrows;   // zeros for a row outside X, whatever W's scale
-            const double y = there ? (double)sum * g.ws[(int64_t)t.e * N + col0 + c] * g.xs[at] : 0.0;
-            Y[r * g.ldy + c] = (T)(float)y;
+            Y[r * g.ldy + c] = (T)(there ? q8_result(sum, g.ws[(int64_t)t.e * N + col0 + c], g.xs[at]) : 0.0f);
         }
     }
 }

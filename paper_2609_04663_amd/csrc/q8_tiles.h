@@ -8,11 +8,8 @@
 // are overwritten with zeros (those of W may then hold anything; one barrier more for
 // a tile).
 //
-// y = x's scale times w's scale times the sum, rounded three times in FP32 (the sum, two
-// products), then to the type.  In a tile where a scale of w could take the product with a
-// sum out of range, mantissas are multiplied and exponents added.  Tiles whose columns all
-// exist, and that need nothing of the kind, are stored without checks (131072 rows below:
-// 336 -> 309 us).
+// Results as q8_result forms them.  Tiles whose columns and rows of X all exist, and none of
+// whose scales is extreme, are stored without checks (131072 rows below: 336 -> 309 us).
 //
 // Tiles of 256 hold one workgroup to a CU; of tiles of 128, a quarter of the accumulators each,
 // two share one, or one has four stages, three k-blocks of copies in flight, where there are no
@@ -188,21 +185,23 @@ struct Q8Source {
         const Scales<TILE> &s = scales[turn];
         const int rows = (int)(now.end - now.first), cols = g.N - now.col * TILE;
         if (SUMS) {
-            if (cols >= TILE) store_rows<true>(acc, s, rows, cols);
-            else store_rows<false>(acc, s, rows, cols);
+            if (cols >= TILE) store_rows<PLAIN>(acc, s, rows, cols);
+            else store_rows<CHECKED>(acc, s, rows, cols);
             return;
         }
-        bool special = cols < TILE;
+        bool special = cols < TILE, extreme = false;
 #pragma unroll
         for (int i = lane; i < RB * 32; i += 64) {
-            const float m = fabsf(s.w[(wave & 1) * RB * 32 + i]);
-            special |= !s.there[(wave >> 1) * RB * 32 + i] || m > 0x1p96f || (m < 0x1p-126f && m > 0.0f);
+            special |= !s.there[(wave >> 1) * RB * 32 + i];
+            extreme |= q8_extreme(s.w[(wave & 1) * RB * 32 + i]);
         }
-        if (__any(special)) store_rows<false>(acc, s, rows, cols);
-        else store_rows<true>(acc, s, rows, cols);
+        if (__any(extreme)) store_rows<EXTREME>(acc, s, rows, cols);
+        else if (__any(special)) store_rows<CHECKED>(acc, s, rows, cols);
+        else store_rows<PLAIN>(acc, s, rows, cols);
     }
-    // PLAIN: every column exists, and nothing is special
-    template <bool PLAIN>
+    // PLAIN: every column and row of X exists; EXTREME: scales may be, else none is
+    enum How { PLAIN, CHECKED, EXTREME };
+    template <How HOW>
     __device__ __forceinline__ void store_rows(const i32x16 (&acc)[RB][RB], const Scales<TILE> &s, int rows,
                                                int cols) const {
         typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -214,7 +213,7 @@ struct Q8Source {
             if (row >= rows) continue;
             Out *const p = Y + row * g.ldy + (sizeof(T) == 4 ? 4 : 8) * h;
             const float x = SUMS ? 1.0f : s.x[row];
-            const bool keep = PLAIN || SUMS || s.there[row];    // zeros for a row outside X, whatever W's scale
+            const bool keep = HOW == PLAIN || SUMS || s.there[row];    // zeros for a row outside X, whatever W's scale
 #pragma unroll
             for (int j = 0; j < RB; ++j) {
                 __builtin_amdgcn_sched_barrier(0);          // few values in flight: no registers to spare
@@ -226,22 +225,22 @@ struct Q8Source {
                     float y[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float sum = (float)acc[i][j][r + k], m = w[k / 4][k % 4];
+                        const int sum = acc[i][j][r + k];
+                        const float m = w[k / 4][k % 4];
                         if constexpr (SUMS)
-                            y[k] = __int_as_float(acc[i][j][r + k]);
-                        else if constexpr (PLAIN)
-                            y[k] = sum * m * x;
+                            y[k] = __int_as_float(sum);
+                        else if constexpr (HOW == EXTREME)
+                            y[k] = q8_result(sum, m, x);
                         else
-                            y[k] = ldexpf(sum * __builtin_amdgcn_frexp_mantf(m) * __builtin_amdgcn_frexp_mantf(x),
-                                          __builtin_amdgcn_frexp_expf(m) + __builtin_amdgcn_frexp_expf(x));
+                            y[k] = (float)sum * m * x;          // the same
                     }
-                    store8<PLAIN>(p + col, keep, cols - col0 - col, y);
+                    store8<HOW == PLAIN>(p + col, keep, cols - col0 - col, y);
                 }
             }
         }
     }
     // y: columns 4 h .. 4 h + 3 and 8 + 4 h .. of 16, of which `cols` exist; p: the lane's first
-    template <bool PLAIN>
+    template <bool WHOLE>
     __device__ __forceinline__ void store8(Out *p, bool keep, int cols, float (&y)[8]) const {
         if constexpr (sizeof(T) == 4) {
             const int first = 4 * (lane >> 5);
@@ -250,7 +249,7 @@ struct Q8Source {
                 float v[4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) v[k] = keep ? y[4 * q + k] : 0.0f;
-                if (PLAIN || first + 8 * q + 4 <= cols) {
+                if (WHOLE || first + 8 * q + 4 <= cols) {
                     store_f32<4>(p + 8 * q, v);
                 } else {
 #pragma unroll
@@ -272,7 +271,7 @@ struct Q8Source {
             if (!keep) w = u32x4{};
             const frag<T> f = __builtin_bit_cast(frag<T>, w);
             const int first = 8 * (lane >> 5);
-            if (PLAIN || first + 8 <= cols) {
+            if (WHOLE || first + 8 <= cols) {
                 *reinterpret_cast<vec<T, 8> *>(p) = f;
             } else {
 #pragma unroll
