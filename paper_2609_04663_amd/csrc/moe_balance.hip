@@ -57,7 +57,7 @@ __device__ inline Span span_of(const int *__restrict__ starts, int S, int64_t T,
 }
 
 // Where the joining kernel finds a workgroup's sums: E probabilities and E counts, each in
-// a row of a multiple of four, then the sum of z^2 and the tokens.
+// a row of a multiple of four, then the sum of z^2 (FP64) and the tokens.
 __host__ __device__ constexpr int padded(int E) { return (E + 3) & ~3; }
 __host__ __device__ constexpr int64_t sums_of(int E) { return 2 * padded(E) + 4; }
 
@@ -149,7 +149,7 @@ template <typename T, int LANES, int V>
 __global__ __launch_bounds__(THREADS, V <= 16 ? 8 : 4) void balance_kernel(BalanceLoss b, int span, float *__restrict__ sums) {
     __shared__ float part[WAVES][LANES * V];
     __shared__ int count[ROUTE_EXPERTS], n_of[WAVES];
-    __shared__ float z_of[WAVES];
+    __shared__ double z_of[WAVES];
     constexpr int GROUPS = THREADS / LANES;
     const int tid = threadIdx.x, sub = tid % LANES, lane = tid & 63, wave = tid >> 6, E = b.E;
     Span at;
@@ -164,7 +164,8 @@ __global__ __launch_bounds__(THREADS, V <= 16 ? 8 : 4) void balance_kernel(Balan
     __syncthreads();
     const T *const logits = static_cast<const T *>(b.logits);
     const int64_t last = at.end - 1;
-    float acc[V] = {}, z = 0.0f;
+    float acc[V] = {};
+    double z = 0;                                           // FP32 does not hold the squares of all z
     int n = 0;
     int64_t t = at.first + tid / LANES;
     for (int64_t i = tid, choices = (at.end - at.first) * b.k; i < choices; i += THREADS) {
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(THREADS, V <= 16 ? 8 : 4) void balance_kernel(Balan
         if (t > last) continue;                             // the group's last load stands in
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] += x[i];
-        z += lse * lse;
+        z += (double)lse * lse;
         n += live;
     }
     // over the groups of the wave, then over the waves
@@ -217,8 +218,8 @@ __global__ __launch_bounds__(THREADS, V <= 16 ? 8 : 4) void balance_kernel(Balan
         out[padded(E) + tid] = __int_as_float(tid < E ? count[tid] : 0);
     }
     if (tid == 0) {
-        out[2 * padded(E)] = (float)zs;
-        out[2 * padded(E) + 1] = __int_as_float(ns);
+        *reinterpret_cast<double *>(out + 2 * padded(E)) = zs;
+        out[2 * padded(E) + 2] = __int_as_float(ns);
     }
 }
 
@@ -241,8 +242,9 @@ __global__ __launch_bounds__(THREADS) void balance_join_kernel(BalanceLoss b, in
     double p[4] = {}, z = 0;
     int c[4] = {}, n = 0;
     for (int i = tid; i < spans; i += THREADS) {
-        z += from[i * stride + 2 * padded(E)];
-        n += __float_as_int(from[i * stride + 2 * padded(E) + 1]);
+        const float *const last = from + i * stride + 2 * padded(E);
+        z += *reinterpret_cast<const double *>(last);
+        n += __float_as_int(last[2]);
     }
     if (e < E)
         for (int i0 = tid / W; i0 < spans; i0 += AHEAD * G) {
