@@ -315,8 +315,9 @@ __global__ __launch_bounds__(256) void balance_grad_kernel(BalanceGrad b, int sp
     }
     choices = over_lanes<LANES>(choices, [](float a, float b) { return a + b; });
     const int n = none ? 0 : b.tokens[s];
-    const float per = n > 0 ? 1.0f / n : 0.0f, dl = n > 0 ? b.dloss[s] * E * per : 0.0f;
-    const float dz = n > 0 && b.dzloss ? b.dzloss[s] * 2.0f * per : 0.0f;
+    // (a token's share first: dloss E may leave FP32's range where dloss E / n does not)
+    const float per = n > 0 ? 1.0f / n : 0.0f, dl = n > 0 ? b.dloss[s] * (E * per) : 0.0f;
+    const float dz = n > 0 && b.dzloss ? b.dzloss[s] * (2.0f * per) : 0.0f;
     const float share = choices > 0.0f ? 1.0f / choices : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) f[i] *= share;

@@ -5,6 +5,9 @@ import math
 import pytest
 import torch
 
+import _moe as M
+import _q8 as Q
+
 pytestmark = pytest.mark.gpu
 
 
@@ -38,3 +41,19 @@ def test_mean_square_out_of_the_range(emu):
     x = torch.full((300, 8), 2e19)
     b = emu.moe_balance(x.cuda(), torch.zeros((300, 1), dtype=torch.int32).cuda())
     assert float(b.zloss) == math.inf
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("dl,dz", [(1e38, 0.0), (1.0, 3e38), (-3e38, -3e38)])
+def test_gradients_of_large_losses(emu, kind, dl, dz):
+    """dloss E and 2 dzloss are beyond the range, a token's share of them is not."""
+    gen = torch.Generator().manual_seed(4)
+    T, E, k = 2000, 64, 4
+    x = (torch.randn((T, E), generator=gen) / 4).to(M.TYPES[kind])
+    ids = torch.topk(x.float(), k).indices.int().contiguous()
+    b = emu.moe_balance(x.cuda(), ids.cuda())
+    dl, dz = torch.tensor([dl]), torch.tensor([dz])
+    ref, bar = Q.balance_grad(x, b.counts.cpu().long(), b.tokens.cpu(), dl, dz, None)
+    assert (ref.abs() < 3e37).all() and (ref.abs() > 1e30).any()
+    got = emu.moe_balance_grad(x.cuda(), b.counts, b.tokens, dl.cuda(), dz.cuda())
+    M.check(got, ref, bar + M.rounded(ref, M.TYPES[kind]))
