@@ -279,10 +279,8 @@ int emu_q8_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, const int8_t 
     if (R > 0 && N > 0 && (!Y || (E > 0 && ((XR > 0 && !xscales) || !wscales || (K > 0 && ((XR > 0 && !X) || !W))))))
         return api_fail(EMU_EINVAL, "NULL pointer");
     if (int rc = check_lds({ldx, ldw, ldy})) return rc;
-    // workgroups of 512 threads: on tiles of 16 x 64 or more where the rows are few, else of 128 x 128
-    const int64_t tiles = R <= FEW_ROWS * E ? row_blocks_bound(R, E, 16) * ((N + 63) / 64)
-                                            : row_blocks_bound(R, E, 128) * ((N + 127) / 128);
-    if (tiles > MAX_TILES / 2) return api_fail(EMU_EINVAL, "product too large");
+    // an expert's tiles, of 16 x 16 or more, are numbered in 31 bits: refused are Ys of 2^38 entries and more
+    if ((R / 16 + 1) * ((N + 15) / 16) > MAX_ROWS) return api_fail(EMU_EINVAL, "product too large");
     api_clear_error();
     if (R == 0 || N == 0) return EMU_OK;
     const Q8Gemm g = {dtype, E, (int)N, (int)K, R, XR, X, W, xscales, wscales, Y, ldx, ldw, stride, ldy, offsets,

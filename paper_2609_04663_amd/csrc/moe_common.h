@@ -238,7 +238,7 @@ struct RowTiles {
         if (e > E) return 0;
         int64_t lo, hi;
         expert_rows(offsets, E, R, e, lo, hi);
-        return ((int)(hi - lo) + rows - 1) / rows;
+        return (int)(((unsigned)(hi - lo) + rows - 1) / rows);
     }
     __device__ __forceinline__ RowTiles(const int *offsets_, int E_, int64_t R_, int rows_, int cols_)
         : offsets(offsets_), E(E_), rows(rows_), cols(cols_), R(R_) {

@@ -10,6 +10,7 @@ namespace {
 
 constexpr int64_t OFFSETS = (int64_t)1 << 32;        // what a copy's 32-bit offset spans
 constexpr int64_t MOST_COPIED = (int64_t)1 << 33;    // bytes of workspace for copies
+constexpr int64_t MOST_TILES = (int64_t)1 << 28;     // a workgroup of 256 takes 32: fewer than 2^32 threads
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 int64_t up(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
@@ -70,11 +71,11 @@ hipError_t copy(const Copied &x, char *to_x, const Copied &w, char *to_w, hipStr
     return hipGetLastError();
 }
 
-// The kernel of q8_tiles.h: rows of whole 16-byte chunks, and offsets of 32 bits.
+// The kernel of q8_tiles.h: rows of whole 16-byte chunks, offsets of 32 bits, and a launch that fits.
 bool fits_tiles(const Q8Gemm &g) {
     return g.K > 0 && g.K % 16 == 0 && g.E > 0 && aligned16(g.X) && aligned16(g.W) && g.ldx % 16 == 0 &&
            g.ldw % 16 == 0 && g.sw % 16 == 0 && (g.rows ? g.xrows : 256) * g.ldx < OFFSETS && 256 * g.ldw < OFFSETS &&
-           (!g.rows || g.xrows > 0);
+           (!g.rows || g.xrows > 0) && row_blocks_bound(g.R, g.E, 128) * ((g.N + 127) / 128) <= MOST_TILES;
 }
 
 // Times, us, that the choice between the two kernels goes by.  Measured, that for few rows

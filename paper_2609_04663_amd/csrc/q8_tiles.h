@@ -105,8 +105,8 @@ struct Q8Source {
             const int l = lane_here();
 #pragma unroll
             for (int c = 0; c < A::COPIES; ++c) {
-                const int r = (int)next.first + A::row_of(c, wave, l);
-                raw[c] = g.rows[r < next.end ? r : (int)next.end - 1];
+                const unsigned r = (unsigned)next.first + A::row_of(c, wave, l), end = (unsigned)next.end;
+                raw[c] = g.rows[r < end ? r : end - 1];
             }
         }
     }
