@@ -25,16 +25,16 @@ import paper_2609_04663_amd as emu  # noqa: E402
 
 class MoE(torch.autograd.Function):
     """y of tokens x (T x D) for the router Wr (D x E, float32) and the experts'
-    W1 (E x H x D) and W2 (E x D x H), k experts a token; the router's losses."""
+    W1 (E x H x D) and W2 (E x D x H), k experts a token; the router's losses, if asked for."""
 
     @staticmethod
-    def forward(ctx, x, Wr, W1, W2, k, scope):
+    def forward(ctx, x, Wr, W1, W2, k, scope, losses):
         logits = emu.sgemm(x.float(), Wr)
         r = emu.moe_route(logits, k, scope)
         h = emu.grouped_gemm(x, W1, r.offsets, transb="T", rows=r.rows)
         a = torch.nn.functional.silu(h)
         z = emu.grouped_gemm(a, W2, r.offsets, transb="T")
-        b = emu.moe_balance(logits, r.ids)
+        b = emu.moe_balance(logits, r.ids) if losses else emu.Balance(None, None, None, None)
         ctx.save_for_backward(x, Wr, W1, W2, logits, h, a, z, b.counts, b.tokens, *r)
         ctx.scope = scope
         ctx.set_materialize_grads(False)
@@ -44,30 +44,36 @@ class MoE(torch.autograd.Function):
     def backward(ctx, dy, dloss, dzloss):
         x, Wr, W1, W2, logits, h, a, z, counts, tokens, *r = ctx.saved_tensors
         r = emu.Routing(*r)
-        dy = x.new_zeros(x.shape) if dy is None else dy
-        dz, dweights = emu.moe_combine_grad(dy.contiguous(), z, r.slots, r.weights, r.rows)
-        dW2 = emu.grouped_wgrad(a, dz, r.offsets, transb="T")
-        da = emu.grouped_gemm(dz, W2, r.offsets)
-        s = torch.sigmoid(h.float())
-        dh = (da.float() * s * (1 + h.float() * (1 - s))).to(h.dtype)
-        dW1 = emu.grouped_wgrad(x, dh, r.offsets, transb="T", rows=r.rows)
-        dx = emu.moe_combine(emu.grouped_gemm(dh, W1, r.offsets), r.slots)     # each token's rows
-        dlogits = emu.moe_route_grad(logits, r.ids, r.weights, dweights, ctx.scope)
+        dx = dW1 = dW2 = dlogits = None
+        if dy is not None:
+            dz, dweights = emu.moe_combine_grad(dy.contiguous(), z, r.slots, r.weights, r.rows)
+            dW2 = emu.grouped_wgrad(a, dz, r.offsets, transb="T")
+            da = emu.grouped_gemm(dz, W2, r.offsets)
+            s = torch.sigmoid(h.float())
+            dh = (da.float() * s * (1 + h.float() * (1 - s))).to(h.dtype)
+            dW1 = emu.grouped_wgrad(x, dh, r.offsets, transb="T", rows=r.rows)
+            dx = emu.moe_combine(emu.grouped_gemm(dh, W1, r.offsets), r.slots)  # each token's rows
+            dlogits = emu.moe_route_grad(logits, r.ids, r.weights, dweights, ctx.scope)
         if dloss is not None or dzloss is not None:
             dloss = counts.new_zeros(1, dtype=torch.float32) if dloss is None else dloss
-            dlogits = dlogits + emu.moe_balance_grad(logits, counts, tokens, dloss, dzloss)
+            of_losses = emu.moe_balance_grad(logits, counts, tokens, dloss, dzloss)
+            dlogits = of_losses if dlogits is None else dlogits + of_losses
+        if dlogits is None:
+            return (None,) * 7
         dWr = emu.sgemm_ex(x.float(), dlogits, transa="T")
-        dx = dx + emu.sgemm_ex(dlogits, Wr, transb="T").to(dx.dtype)
-        return dx, dWr, dW1, dW2, None, None
+        of_logits = emu.sgemm_ex(dlogits, Wr, transb="T").to(x.dtype)
+        if dy is None:                      # the losses alone do not reach the experts
+            return of_logits, dWr, torch.zeros_like(W1), torch.zeros_like(W2), None, None, None
+        return dx + of_logits, dWr, dW1, dW2, None, None, None
 
 
 def moe_with_losses(x, Wr, W1, W2, k, scope="chosen"):
     """y, the balance loss and the squared log of the router's softmax sum (one each)."""
-    return MoE.apply(x, Wr, W1, W2, k, scope)
+    return MoE.apply(x, Wr, W1, W2, k, scope, True)
 
 
 def moe(x, Wr, W1, W2, k, scope="chosen"):
-    return moe_with_losses(x, Wr, W1, W2, k, scope)[0]
+    return MoE.apply(x, Wr, W1, W2, k, scope, False)[0]
 
 
 class Served:
