@@ -227,9 +227,9 @@ int emu_set_sgemm_split(int mode);
    stream, no host synchronisation (but where the workspace grows).  It is used by emu_moe_route
    (more than 64 tokens), emu_moe_balance (more than 256), emu_q4_gemm (a reduction that is
    split), the grouped products (16-bit operands that are copied to 16-byte alignment first,
-   sums of few matrices in pieces) and emu_q8_gemm (operands that are copied); all but the first
-   two do without it where it cannot grow (no memory beside what is held, EMU_WORKSPACE_LIMIT, a
-   stream under capture).
+   sums of few matrices in pieces) and emu_q8_gemm (operands that are copied, a reduction of one
+   matrix that is split; at most 8 GiB); all but the first two do without it where it cannot
+   grow (no memory beside what is held, EMU_WORKSPACE_LIMIT, a stream under capture).
    offsets: E + 1 entries, rows [offsets[e], offsets[e + 1]) belong to expert e
    (offsets[0] counts as 0); an expert may have none.  Rows from offsets[E] on
    belong to no expert: their outputs are zero and their inputs are not used.
@@ -362,7 +362,9 @@ int emu_q8_unpack(int dtype, int64_t rows, int64_t K, const int8_t *Q, int64_t l
    a row of Y depend on its own operands alone, not on the other rows or the workspace.  A row
    of Y whose row of X does not exist is zeros.  Operands whose rows are not multiples of 16 bytes are
    copied to the workspace first where there are many rows; without workspace, and for
-   few rows, they are read as they are. */
+   few rows, they are read as they are.  A long reduction of one matrix (K from 1024 on) with
+   few results is split over workgroups, whatever the alignment: the 32-bit sums, 2 to 16
+   for a result, are in the workspace; without it the reduction is in one piece. */
 int emu_q8_gemm(int dtype, int E, int64_t R, int64_t N, int64_t K, const int8_t *X, int64_t ldx,
                 const float *xscales, int64_t XR, const int32_t *rows, const int8_t *W, int64_t ldw,
                 int64_t stride, const float *wscales, const int32_t *offsets, void *Y, int64_t ldy);

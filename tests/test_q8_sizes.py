@@ -31,7 +31,9 @@ for dtype in (0, 1):
                                                p, p, i(N))
                         result.append([dtype, E, R, N, K, shared, rc,
                                        [l[2:6] for l in L.log() if l[0] == "launch"]])
+result.append(L.emu.emu_workspace_bytes())
 """)
+    assert 0 < out.pop() <= 1 << 33                         # the header's limit of what a call asks for
     taken = 0
     for dtype, E, R, N, K, shared, rc, launches in out:
         assert rc in (0, 1)
