@@ -7,9 +7,10 @@
 // its row or column twice, 64 apart.  The waves of a workgroup take neighbouring runs of
 // 128 and add up their 32-bit sums in LDS at the end.
 //
-// One row of 4096 x 4096 takes 6.2 us (2.7 TB/s; a launch, and four rounds of loads that wait for
-// one another), 8 rows over 64 experts of 2048 x 2048 9.8 with the call.  More rounds in flight
-// gained nothing (16 rows of 8192 x 8192 18.1 and, with six, 19.4 us).
+// One row of 4096 x 4096 takes 6.0 us (2.8 TB/s; a launch, and four rounds of loads that wait for
+// one another), 8 rows over 64 experts of 2048 x 2048 9.8 with the call.  Six rounds in flight
+// instead of two spilled and lost where they were tried (16 rows of 8192 x 8192 in 16 columns 18.1
+// and 19.4 us); one row alone, which holds 67 of its 128 registers, was not.
 #include "emu_internal.h"
 #include "moe.h"
 #include "moe_common.h"
@@ -157,7 +158,10 @@ __device__ __forceinline__ void q8_few_tile(const Q8Gemm &g, const RowTile &t, i
     }
 }
 
-// Workgroups to a CU, by the registers that the kernel needs.
+// Workgroups to a CU, by the registers that the kernel needs.  With four sets of one kind and one
+// of the other, two workgroups spill 5 to 8: one to a CU without spills takes 23.5 us instead of
+// 24.8 for 16 rows of 16384 x 8192 in 64 columns, but 26.0 instead of 23.8 for 64 of 8192 x 4096 in
+// 16, 43 instead of 40 for 64 of 8192 x 8192.
 constexpr int few_per_cu(int mt, int nt, bool shift) { return mt + nt >= (shift ? 4 : 6) ? 1 : 2; }
 
 // T int: the sums of a split.
@@ -178,8 +182,10 @@ __global__ __launch_bounds__(THREADS, 2 * few_per_cu(MT, NT, SHIFT)) void q8_few
 }  // namespace
 
 // Rows and columns of a tile, in sixteens: rows for those of an expert on average, 64 at most;
-// as many columns as fill the chip (32 rows of 8192 x 4096, 16, 32 and 64 columns: 14.1, 11.5
-// and 14.9 us; 64 rows 23, 16 and 20; 16 rows of 8192 x 8192 18, 20 and 21).
+// as many columns as fill the chip.  Calls with 16, 32 and 64 columns: 16 rows of 8192 x 4096 10.5, 9.0
+// and 12.8 us, of 16384 x 8192 31.5, 32.9 and 24.8; 32 rows of 8192 x 4096 14.1, 10.7 and 14.8, of 8192 x
+// 8192 24.4, 21.9 and 25.0; 64 rows of 8192 x 4096 23.8, 16.3 and 19.8.  At 8192 x 8192 the rule's
+// 32 columns are not the best for 16 rows (18.0, 20.5 and 21.4) or one (14.3, 19.8 and 18.5).
 static int row_sets(const Q8Gemm &g) {
     return g.R <= 16 * (int64_t)g.E ? 1 : (g.R <= 32 * (int64_t)g.E ? 2 : 4);
 }

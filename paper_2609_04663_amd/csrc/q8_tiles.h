@@ -16,9 +16,9 @@
 // more tiles than CUs.  Those read fragments two sub-steps ahead: a sub-step of theirs is four
 // MFMAs long, less than the latency of an LDS read under load.
 //
-// Measured in bfloat16: 8192 x 8192 x 8192 442 to 462 us (2.4 to 2.5 POP/s, MFMA busy for 64 % of the
-// cycles at 1.8 GHz, the power limit); 131072 gathered rows over 64 experts of 1024 x 2048 299 to
-// 306 us, of which forming the results is 28 and storing them 34.  A k-block of a tile of 128
+// Measured in bfloat16: 8192 x 8192 x 8192 439 to 466 us (2.4 to 2.5 POP/s, MFMA busy for 64 % of the
+// cycles at 1.8 GHz, the power limit); 131072 gathered rows over 64 experts of 1024 x 2048 295 to
+// 308 us, of which forming the results is 28 and storing them 34.  A k-block of a tile of 128
 // takes 0.45 us (1000 cycles) however few run, its MFMAs 512 cycles: the LDS takes 32 KB of
 // copies (as if at 64 bytes a cycle) and gives 64 KB of fragments.
 #pragma once
